@@ -9,7 +9,8 @@
  * Beyond that path, further down in this header: incremental updates of a tree, the
  * coefficient route of Def. 4.1 as printed (interpolation, Algorithm 1), and two parts
  * that run on the host only, as the paper's verifier has no GPU: verification with the
- * pairing and the layer selection of Sec. 4.3.
+ * pairing and the layer selection of Sec. 4.3.  Beside the quantisation of activations stand the
+ * layer operators: 8-bit checkpoints, norms, matrix products, and their gradients.
  *
  * Conventions
  *   - Every function returns TC_OK (0) or a negative TC_ERR_* code; nothing
@@ -64,7 +65,8 @@ extern "C" {
 #define TC_I8 1  /* int8_t   */
 #define TC_I16 2 /* int16_t  */
 #define TC_FR 3  /* 32-byte canonical Fr elements */
-#define TC_F16 4 /* IEEE binary16 (source type of tc_encode_tensor only) */
+#define TC_F16 4 /* IEEE binary16 (source type of tc_encode_tensor, tensors of the layer operators) */
+#define TC_BF16 5 /* bfloat16 (tensors of the layer operators only) */
 
 typedef struct tc_ctx tc_ctx;
 typedef struct tc_srs tc_srs;
@@ -224,6 +226,77 @@ int tc_encode_tensor_scaled(tc_ctx* ctx, const void* d_src, int src_dtype, size_
  * Results are those of the two calls per tensor, bit for bit.  Asynchronous on the context's stream. */
 int tc_encode_batch_scaled(tc_ctx* ctx, int count, const void* const* d_src, const size_t* n, float* d_inv_scale,
                            void* const* d_dst);
+
+/* ---- layer operators: the passes that make the tensors, and their gradients -----------------------
+ *
+ * A prover commits to what a layer's products and norms have made.  These calls are those passes, for tensors that stay
+ * where the commitment reads them: 16-bit activations, weights in 16 bits or as the committed int8 rows, and activations
+ * kept for a backward pass in 8 bits, in the form that tc_commit takes (TC_I8), so that a commitment binds the very bytes
+ * that the gradients were taken from.
+ *
+ * All of them are asynchronous on the context's stream, allocate nothing, read nothing back and may be captured into a
+ * graph; scratch memory is the caller's (the *_workspace calls say how much).  The same call on the same data gives the same bytes, every time: no
+ * sum depends on the order in which workgroups run.  Sums, statistics and products are held in 32 bits; results are
+ * rounded once to their type.  Outputs may not overlap inputs or one another, but for: y in the place of the residual
+ * (tc_linear), y in the place of x (tc_norm), dx in the place of dy (tc_norm_backward), dz in the place of dy
+ * (tc_linear_backward).  Two calls that overlap in time (on several streams, or as replayed graphs) need a workspace each. */
+
+/* A view of device memory: rows x cols elements, row r at d_data + r * ld elements.  d_scale: for TC_I8, one float32 for
+ * each row, the entry standing for d_scale[r] * q; not looked at for the other types.  Any alignment of whole elements
+ * and any ld >= cols will do; 16-byte aligned rows of a multiple of 8 elements are what the kernels are fast on.
+ * What lies between the rows (cols .. ld - 1) is neither read as data nor written.  rows = 0 is an empty view (d_data may be NULL). */
+typedef struct tc_matrix {
+    void* d_data;
+    float* d_scale;
+    uint32_t rows, cols;
+    uint64_t ld;
+    int dtype; /* TC_F16, TC_BF16 or TC_I8 */
+} tc_matrix;
+#define TC_LAYER_MAX_COLS (1u << 20)       /* columns of a view */
+#define TC_LAYER_MAX_LD (1ull << 31)       /* elements from one row to the next */
+#define TC_NORM_MAX_COLS (1u << 15)        /* columns of a row that is normalised */
+
+/* 8-bit checkpoints.  src: 16-bit rows; dst: TC_I8 rows of the same shape with d_scale.  With amax the largest magnitude among the
+ * finite values of row r:  scale[r] = float32(amax / 127),  q = 127 x / amax rounded to the nearest whole number, half
+ * to even, in exact arithmetic (no step of it is rounded on the way: the bytes are the same on every machine).
+ * Infinities become +-127 and NaNs 0, as in tc_quant_scale; a row without a non-zero finite value has scale 0 and its finite entries are 0. */
+int tc_checkpoint_encode(tc_ctx* ctx, const tc_matrix* src, const tc_matrix* dst);
+/* dst (16 bits) = scale * q */
+int tc_checkpoint_decode(tc_ctx* ctx, const tc_matrix* src, const tc_matrix* dst);
+
+/* Norms over the last axis.  TC_NORM_LAYER: mu the mean, rstd = 1 / sqrt(mean((x - mu)^2) + eps); TC_NORM_RMS: mu = 0.
+ * y = (x - mu) rstd gamma + beta.  x: 16 bits, or TC_I8 (a checkpoint, whose norm is recomputed); y: 16 bits; d_gamma, d_beta: cols values of
+ * y's type, either may be NULL (1, 0).  d_mean, d_rstd: rows float32 each, for the backward pass, or NULL.  0 < eps < 1. */
+#define TC_NORM_LAYER 0
+#define TC_NORM_RMS 1
+int tc_norm(tc_ctx* ctx, int kind, const tc_matrix* x, const void* d_gamma, const void* d_beta, float eps, const tc_matrix* y,
+            float* d_mean, float* d_rstd);
+/* Its gradient, with xh = (x - mu) rstd and g = dy gamma:
+ *   dx = rstd (g - mean(g) - xh mean(g xh))   (without mean(g) for TC_NORM_RMS),   dgamma = sum over rows of dy xh,   dbeta = sum of dy.
+ * x: what the forward pass read, in 16 bits or as a checkpoint; d_mean (ignored for TC_NORM_RMS) and d_rstd: what it wrote.
+ * dx has dy's type; d_dgamma, d_dbeta: cols float32 each; any of the three outputs may be NULL. */
+int tc_norm_backward(tc_ctx* ctx, int kind, const tc_matrix* dy, const tc_matrix* x, const void* d_gamma, const float* d_mean,
+                     const float* d_rstd, const tc_matrix* dx, float* d_dgamma, float* d_dbeta, void* d_workspace, size_t workspace_bytes);
+int tc_norm_backward_workspace(uint32_t rows, uint32_t cols, size_t* bytes);
+
+/* z = x w^T + bias,  y = act(z) + residual.  x: rows x in, 16 bits; w: out x in, of x's type or TC_I8 with its scales (the
+ * rows as they are committed); d_bias: out values of x's type or NULL; residual and z: rows x out of x's type or NULL; y the same.
+ * TC_ACT_GELU is z Phi(z), Phi the normal distribution's integral; TC_ACT_SILU is z / (1 + exp(-z)). */
+#define TC_ACT_NONE 0
+#define TC_ACT_RELU 1
+#define TC_ACT_GELU 2
+#define TC_ACT_SILU 3
+int tc_linear(tc_ctx* ctx, const tc_matrix* x, const tc_matrix* w, const void* d_bias, int activation, const tc_matrix* residual,
+              const tc_matrix* y, const tc_matrix* z, void* d_workspace, size_t workspace_bytes);
+int tc_linear_workspace(uint32_t rows, uint32_t in, uint32_t out, size_t* bytes);
+/* Its gradients:  dz = dy act'(z),  dx = dz w,  dw = dz^T x,  dbias = sum over rows of dz (relu'(0) = 0; the residual's gradient is dy itself).
+ * z and x: as the forward pass had them, in 16 bits or as checkpoints; w as there.  With an activation z and dz are needed; without one
+ * both must be NULL and dz is dy.  x may be NULL without dw, w without dx.  dz, dx, dw have dy's type; d_dbias: out float32.  dx, dw
+ * and d_dbias may be NULL. */
+int tc_linear_backward(tc_ctx* ctx, const tc_matrix* dy, const tc_matrix* x, const tc_matrix* w, int activation, const tc_matrix* z,
+                       const tc_matrix* dz, const tc_matrix* dx, const tc_matrix* dw, float* d_dbias, void* d_workspace,
+                       size_t workspace_bytes);
+int tc_linear_backward_workspace(uint32_t rows, uint32_t in, uint32_t out, size_t* bytes);
 
 /* ---- Com (Def. 4.1, Com) -------------------------------------------------------- */
 

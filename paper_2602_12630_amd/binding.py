@@ -9,7 +9,9 @@ import os
 
 TC_OK = 0
 TC_ERR_ARG, TC_ERR_SHAPE, TC_ERR_RANGE, TC_ERR_NOMEM, TC_ERR_HIP, TC_ERR_VERIFY, TC_ERR_STATE = -1, -2, -3, -4, -5, -6, -7
-TC_I8, TC_I16, TC_FR, TC_F16 = 1, 2, 3, 4
+TC_I8, TC_I16, TC_FR, TC_F16, TC_BF16 = 1, 2, 3, 4, 5
+TC_NORM_LAYER, TC_NORM_RMS = 0, 1
+TC_ACT_NONE, TC_ACT_RELU, TC_ACT_GELU, TC_ACT_SILU = 0, 1, 2, 3
 TC_SRS_SUFFIX, TC_SRS_FIXED_BASE, TC_SRS_MONOMIAL, TC_SRS_OPEN_TABLE = 1, 2, 4, 8
 TC_INTERP_NEWTON, TC_INTERP_GREGORY, TC_INTERP_BARYCENTRIC = 0, 1, 2
 TC_LEAF_ENTRIES, TC_LEAF_TENSORS = 0, 1
@@ -52,6 +54,17 @@ class tc_path(ctypes.Structure):
         ("m", ctypes.c_int * TC_MAX_STEPS),
         ("shape", (ctypes.c_uint32 * TC_MAX_ORDER) * TC_MAX_STEPS),
         ("kappa", (ctypes.c_uint32 * TC_MAX_ORDER) * TC_MAX_STEPS),
+    ]
+
+
+class tc_matrix(ctypes.Structure):
+    _fields_ = [
+        ("d_data", ctypes.c_void_p),
+        ("d_scale", ctypes.c_void_p),
+        ("rows", ctypes.c_uint32),
+        ("cols", ctypes.c_uint32),
+        ("ld", ctypes.c_uint64),
+        ("dtype", ctypes.c_int),
     ]
 
 
@@ -98,6 +111,16 @@ def load_library(path=None):
         "tc_quant_scale": (ctypes.c_int, [vp, vp, ctypes.c_size_t, vp]),
         "tc_encode_tensor_scaled": (ctypes.c_int, [vp, vp, ctypes.c_int, ctypes.c_size_t, vp, vp]),
         "tc_encode_batch_scaled": (ctypes.c_int, [vp, ctypes.c_int, vp, vp, vp, vp]),
+        "tc_checkpoint_encode": (ctypes.c_int, [vp, vp, vp]),
+        "tc_checkpoint_decode": (ctypes.c_int, [vp, vp, vp]),
+        "tc_norm": (ctypes.c_int, [vp, ctypes.c_int, vp, vp, vp, ctypes.c_float, vp, vp, vp]),
+        "tc_norm_backward": (ctypes.c_int, [vp, ctypes.c_int, vp, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t]),
+        "tc_norm_backward_workspace": (ctypes.c_int, [ctypes.c_uint32, ctypes.c_uint32, ctypes.POINTER(ctypes.c_size_t)]),
+        "tc_linear": (ctypes.c_int, [vp, vp, vp, vp, ctypes.c_int, vp, vp, vp, vp, ctypes.c_size_t]),
+        "tc_linear_workspace": (ctypes.c_int, [ctypes.c_uint32, ctypes.c_uint32, ctypes.c_uint32, ctypes.POINTER(ctypes.c_size_t)]),
+        "tc_linear_backward": (ctypes.c_int, [vp, vp, vp, vp, ctypes.c_int, vp, vp, vp, vp, vp, vp, ctypes.c_size_t]),
+        "tc_linear_backward_workspace": (ctypes.c_int, [ctypes.c_uint32, ctypes.c_uint32, ctypes.c_uint32,
+                                                        ctypes.POINTER(ctypes.c_size_t)]),
         "tc_commit": (ctypes.c_int, [vp, vp, vp, ctypes.c_int, vp]),
         "tc_commit_batch": (ctypes.c_int, [vp, ctypes.c_int, ctypes.POINTER(vp), ctypes.POINTER(vp),
                                            ctypes.POINTER(ctypes.c_int), vp]),
@@ -263,6 +286,37 @@ def _ptr(x):
     if hasattr(x, "ctypes"):
         return ctypes.c_void_p(x.ctypes.data)
     return ctypes.c_void_p(int(x))
+
+
+def _nbytes(x):
+    return 0 if x is None else x.numel() * x.element_size()
+
+
+class Matrix:
+    """A view of a 2-D torch tensor (float16, bfloat16 or int8, stride 1 along the rows) for the layer operators; `scale`: for
+    int8, a float32 tensor with one entry for each row.  It keeps the tensors alive and may be used for any number of calls."""
+
+    _DTYPES = {"torch.float16": TC_F16, "torch.bfloat16": TC_BF16, "torch.int8": TC_I8}
+
+    def __init__(self, tensor, scale=None):
+        if tensor.dim() != 2:
+            raise ValueError("a matrix has two axes, this tensor has %d" % tensor.dim())
+        rows, cols = tensor.shape
+        if str(tensor.dtype) not in self._DTYPES:
+            raise ValueError("no matrix of %s" % tensor.dtype)
+        if cols > 1 and rows and tensor.stride(1) != 1:
+            raise ValueError("the entries of a row must lie side by side")
+        if tensor.dtype.is_floating_point != (scale is None):
+            raise ValueError("int8 rows come with a scale each, 16-bit rows with none")
+        if scale is not None and (str(scale.dtype) != "torch.float32" or tuple(scale.shape) != (rows,) or (rows > 1 and scale.stride(0) != 1)):
+            raise ValueError("the scales are float32, side by side, one for each row")
+        if scale is not None and scale.device != tensor.device:
+            raise ValueError("rows and scales are on different devices")
+        self.tensor, self.scale = tensor, scale
+        ld = tensor.stride(0) if rows > 1 else cols
+        self.view = tc_matrix(tensor.data_ptr() or None, scale.data_ptr() or None if scale is not None else None, rows, cols, ld,
+                              self._DTYPES[str(tensor.dtype)])
+        self._as_parameter_ = ctypes.addressof(self.view)
 
 
 class Srs:
@@ -454,6 +508,49 @@ class Context:
         a_dst = (ctypes.c_void_p * k)(*[_ptr(x).value for x in dsts])
         a_n = (ctypes.c_size_t * k)(*[int(v) for v in ns])
         self._check(self.lib.tc_encode_batch_scaled(self.handle, k, a_src, a_n, _ptr(inv_scales_dev), a_dst))
+
+    # -- layer operators -----------------------------------------------------------------------
+    # dy, x, w, y, z, residual, dx, dz, dw, src and dst are Matrix objects; gamma, beta, bias, mean, rstd, dgamma, dbeta, dbias are
+    # contiguous tensors (16-bit parameters of the activations' type, float32 statistics and sums).
+    def checkpoint_encode(self, src, dst):
+        """dst (int8 rows, scales) = the 8-bit form of src's rows"""
+        self._check(self.lib.tc_checkpoint_encode(self.handle, src, dst))
+
+    def checkpoint_decode(self, src, dst):
+        self._check(self.lib.tc_checkpoint_decode(self.handle, src, dst))
+
+    def norm(self, kind, x, gamma, beta, eps, y, mean=None, rstd=None):
+        self._check(self.lib.tc_norm(self.handle, kind, x, _ptr(gamma), _ptr(beta), eps, y, _ptr(mean), _ptr(rstd)))
+
+    def norm_backward(self, kind, dy, x, gamma, mean, rstd, dx, dgamma, dbeta, workspace):
+        """workspace: a uint8 tensor of norm_backward_workspace(rows, cols) bytes"""
+        self._check(self.lib.tc_norm_backward(self.handle, kind, dy, x, _ptr(gamma), _ptr(mean), _ptr(rstd), dx, _ptr(dgamma),
+                                              _ptr(dbeta), _ptr(workspace), _nbytes(workspace)))
+
+    def linear(self, x, w, y, bias=None, activation=TC_ACT_NONE, residual=None, z=None, workspace=None):
+        """workspace: a uint8 tensor of linear_workspace(rows, in, out) bytes"""
+        self._check(self.lib.tc_linear(self.handle, x, w, _ptr(bias), activation, residual, y, z, _ptr(workspace), _nbytes(workspace)))
+
+    def linear_backward(self, dy, x, w, activation=TC_ACT_NONE, z=None, dz=None, dx=None, dw=None, dbias=None, workspace=None):
+        """workspace: a uint8 tensor of linear_backward_workspace(rows, in, out) bytes"""
+        self._check(self.lib.tc_linear_backward(self.handle, dy, x, w, activation, z, dz, dx, dw, _ptr(dbias), _ptr(workspace),
+                                                _nbytes(workspace)))
+
+    def _workspace(self, call, *sizes):
+        out = ctypes.c_size_t()
+        rc = call(*sizes, ctypes.byref(out))
+        if rc != TC_OK:
+            raise TcError(rc, "workspace of these sizes")
+        return int(out.value)
+
+    def norm_backward_workspace(self, rows, cols):
+        return self._workspace(self.lib.tc_norm_backward_workspace, rows, cols)
+
+    def linear_workspace(self, rows, in_features, out_features):
+        return self._workspace(self.lib.tc_linear_workspace, rows, in_features, out_features)
+
+    def linear_backward_workspace(self, rows, in_features, out_features):
+        return self._workspace(self.lib.tc_linear_backward_workspace, rows, in_features, out_features)
 
     def commit(self, srs, scalars, dtype):
         out = ctypes.create_string_buffer(96)

@@ -1,0 +1,468 @@
+/*
+ * Host side of the layer operators declared in include/tc.h: checks of the arguments and launches of the kernels of layers.h.
+ *
+ * Compiled by hipcc for gfx950 (product) or, with -DTC_HOST_EMU, by g++ with plain loops in the place of the
+ * launches, which only CPU tests of the checks and of the views use.
+ */
+#include <algorithm>
+#include <cmath>
+
+#include "ctx.h"
+#if defined(TC_HOST_EMU)
+#include "layers_emu.h"
+#else
+#include "layers.h"
+#endif
+
+using namespace tc;
+
+namespace {
+
+#define TRY(call)                     \
+    do {                              \
+        int rc_ = (call);             \
+        if (rc_ != TC_OK) return rc_; \
+    } while (0)
+#define REFUSE(code, msg) return ctx_fail(ctx, code, msg)
+
+bool sixteen(int dtype) { return dtype == TC_F16 || dtype == TC_BF16; }
+
+/* a view that the kernels may use: known type, sizes and stride in range, aligned to its elements */
+int check_view(tc_ctx* ctx, const tc_matrix* m, bool eight_allowed) {
+    if (!m) REFUSE(TC_ERR_ARG, "null matrix");
+    if (!sixteen(m->dtype) && !(eight_allowed && m->dtype == TC_I8)) REFUSE(TC_ERR_ARG, "matrix of a type that this argument does not take");
+    if (m->cols == 0 || m->cols > TC_LAYER_MAX_COLS || m->rows > 0x7FFFFFFFu) REFUSE(TC_ERR_SHAPE, "rows or columns out of range");
+    if (m->ld < m->cols || m->ld > TC_LAYER_MAX_LD) REFUSE(TC_ERR_SHAPE, "row stride shorter than a row, or out of range");
+    if (m->rows == 0) return TC_OK;
+    if (!m->d_data) REFUSE(TC_ERR_ARG, "null matrix data");
+    if (sixteen(m->dtype) && ((uintptr_t)m->d_data & 1u)) REFUSE(TC_ERR_ARG, "misaligned matrix");
+    if (m->dtype == TC_I8) {
+        if (!m->d_scale) REFUSE(TC_ERR_ARG, "int8 matrix without its scales");
+        if ((uintptr_t)m->d_scale & 3u) REFUSE(TC_ERR_ARG, "misaligned scales");
+    }
+    return TC_OK;
+}
+int check_shape(tc_ctx* ctx, const tc_matrix* m, uint32_t rows, uint32_t cols) {
+    if (m->rows != rows || m->cols != cols) REFUSE(TC_ERR_SHAPE, "matrices of shapes that do not fit together");
+    return TC_OK;
+}
+int check_type(tc_ctx* ctx, const tc_matrix* m, int dtype) {
+    if (m->dtype != dtype) REFUSE(TC_ERR_ARG, "matrices of different 16-bit types");
+    return TC_OK;
+}
+int check_vector(tc_ctx* ctx, const void* p, unsigned element) {
+    if ((uintptr_t)p & (element - 1)) REFUSE(TC_ERR_ARG, "misaligned vector");
+    return TC_OK;
+}
+int check_workspace(tc_ctx* ctx, const void* ws, size_t have, size_t need) {
+    if (!need) return TC_OK;
+    if (!ws || have < need) REFUSE(TC_ERR_ARG, "workspace missing or too small");
+    if ((uintptr_t)ws & 15u) REFUSE(TC_ERR_ARG, "workspace not aligned to 16 bytes");
+    return TC_OK;
+}
+size_t up(size_t x, size_t a) { return (x + a - 1) / a * a; }
+
+/* rows of the input gradient that one workgroup of its kernel has in flight */
+uint32_t norm_back_sets(uint32_t cols) { return cols <= 512 ? 16 : cols <= 4096 ? 4 : 1; }
+/* workgroups of it: one for each compute unit, each leaves a partial row of gamma's and beta's gradients */
+uint32_t norm_back_groups(uint32_t rows, uint32_t cols) {
+    const uint32_t sets = norm_back_sets(cols);
+    return std::min<uint32_t>(256, (rows + sets - 1) / sets);
+}
+/* sets of rows over which the gradient before the activation is spread: about eight workgroups for each compute unit */
+uint32_t slope_groups(uint32_t rows, uint32_t cols) {
+    const uint32_t strips = (cols + 511) / 512;
+    return std::max<uint32_t>(1, std::min<uint32_t>((2048 + strips - 1) / strips, (rows + 15) / 16));
+}
+/* workspace of the linear gradients: where each part lies */
+struct BackPlan {
+    size_t by_x, by_w, part, m, bytes;
+    uint64_t ld_by;
+};
+BackPlan back_plan(uint32_t rows, uint32_t out) {
+    BackPlan b;
+    b.ld_by = up(out, 8);
+    const size_t scaled = up((size_t)rows * b.ld_by * 2, 256);
+    b.by_x = 0;
+    b.by_w = scaled;
+    b.part = 2 * scaled;
+    b.m = b.part + up((size_t)slope_groups(rows, out) * out * 4, 256);
+    b.bytes = b.m + 256;
+    return b;
+}
+
+}  // namespace
+
+#if !defined(TC_HOST_EMU)
+namespace {
+using namespace tc::layers;
+#define LAUNCH(kernel, grid, block, lds, args)                                              \
+    do {                                                                                    \
+        hipLaunchKernelGGL(kernel, grid, dim3(block), lds, ctx_stream(ctx), args);          \
+        int e_ = (int)hipGetLastError();                                                    \
+        if (e_) return ctx_fail_hip(ctx, e_, "launch of " #kernel);                         \
+    } while (0)
+
+/* sixteen-byte accesses to 16-bit rows, eight-byte ones to int8 rows */
+bool wide(const void* p, uint64_t ld, uint32_t rows, uint32_t cols, int dtype) {
+    const uintptr_t mask = dtype == TC_I8 ? 7u : 15u;
+    return ((uintptr_t)p & mask) == 0 && cols % 8 == 0 && (rows <= 1 || ld % 8 == 0);
+}
+bool wide(const tc_matrix* m) { return wide(m->d_data, m->ld, m->rows, m->cols, m->dtype); }
+
+template <class T, bool WIDE>
+int encode_rows(tc_ctx* ctx, const RowArgs& a) {
+    const uint32_t c = a.cols;
+    if (c <= 512) LAUNCH((checkpoint_encode<T, WIDE, 64, 1>), dim3((a.rows + 3) / 4), 256, 0, a);
+    else if (c <= 2048) LAUNCH((checkpoint_encode<T, WIDE, 256, 1>), dim3(a.rows), 256, 0, a);
+    else if (c <= 4096) LAUNCH((checkpoint_encode<T, WIDE, 256, 2>), dim3(a.rows), 256, 0, a);
+    else if (c <= 8192) LAUNCH((checkpoint_encode<T, WIDE, 256, 4>), dim3(a.rows), 256, 0, a);
+    else if (c <= 16384) LAUNCH((checkpoint_encode<T, WIDE, 256, 8>), dim3(a.rows), 256, 0, a);
+    else LAUNCH((checkpoint_encode<T, WIDE, 1024, 0>), dim3(a.rows), 1024, 0, a);
+    return TC_OK;
+}
+template <class T, bool WIDE>
+int norm_rows(tc_ctx* ctx, const NormArgs& a) {
+    const uint32_t c = a.cols;
+    if (c <= 512) LAUNCH((norm_forward<T, WIDE, 64, 1>), dim3((a.rows + 3) / 4), 256, 0, a);
+    else if (c <= 2048) LAUNCH((norm_forward<T, WIDE, 256, 1>), dim3(a.rows), 256, 0, a);
+    else if (c <= 4096) LAUNCH((norm_forward<T, WIDE, 256, 2>), dim3(a.rows), 256, 0, a);
+    else if (c <= 8192) LAUNCH((norm_forward<T, WIDE, 256, 4>), dim3(a.rows), 256, 0, a);
+    else if (c <= 16384) LAUNCH((norm_forward<T, WIDE, 1024, 2>), dim3(a.rows), 1024, 0, a);
+    else LAUNCH((norm_forward<T, WIDE, 1024, 4>), dim3(a.rows), 1024, 0, a);
+    return TC_OK;
+}
+template <class T, bool WIDE>
+int norm_back_rows(tc_ctx* ctx, const NormBackArgs& a, uint32_t groups) {
+    const uint32_t c = a.cols;
+    const dim3 grid(groups);
+    const size_t lds = norm_back_sets(c) > 1 ? (size_t)c * 4 : 0;
+    if (c <= 512) LAUNCH((norm_backward<T, WIDE, 64, 1>), grid, NORM_BACK_LANES, lds, a);
+    else if (c <= 2048) LAUNCH((norm_backward<T, WIDE, 256, 1>), grid, NORM_BACK_LANES, lds, a);
+    else if (c <= 4096) LAUNCH((norm_backward<T, WIDE, 256, 2>), grid, NORM_BACK_LANES, lds, a);
+    else if (c <= 8192) LAUNCH((norm_backward<T, WIDE, 1024, 1>), grid, NORM_BACK_LANES, lds, a);
+    else if (c <= 16384) LAUNCH((norm_backward<T, WIDE, 1024, 2>), grid, NORM_BACK_LANES, lds, a);
+    else LAUNCH((norm_backward<T, WIDE, 1024, 4>), grid, NORM_BACK_LANES, lds, a);
+    return TC_OK;
+}
+int sum_columns(tc_ctx* ctx, const float* part, uint64_t stride, uint32_t n, uint32_t cols, float* out) {
+    const ColumnSumArgs a{part, out, stride, n, cols};
+    LAUNCH(column_sums, dim3((cols + 63) / 64), 1024, 0, a);
+    return TC_OK;
+}
+template <class T>
+int clear_rows(tc_ctx* ctx, void* out, uint64_t ld, uint32_t rows, uint32_t cols) {
+    const uint64_t n = (uint64_t)rows * cols;
+    hipLaunchKernelGGL(fill_rows<T>, dim3((uint32_t)std::min<uint64_t>(2048, (n + 255) / 256)), dim3(256), 0, ctx_stream(ctx), (T*)out, ld, rows, cols);
+    int e = (int)hipGetLastError();
+    return e ? ctx_fail_hip(ctx, e, "launch of fill_rows") : TC_OK;
+}
+template <class T, bool P_ALONG, bool P_EIGHT, bool Q_ALONG, bool Q_EIGHT, bool FORWARD>
+int multiply(tc_ctx* ctx, const ProductArgs& a) {
+    const uint64_t tiles = (uint64_t)((a.np + 127) / 128) * ((a.nq + 127) / 128);
+    if (tiles > 0x7FFFFFFFu) REFUSE(TC_ERR_SHAPE, "product too large");
+    LAUNCH((product<T, P_ALONG, P_EIGHT, Q_ALONG, Q_EIGHT, FORWARD>), dim3((uint32_t)tiles), 256, 0, a);
+    return TC_OK;
+}
+
+template <class T>
+int run_encode(tc_ctx* ctx, const tc_matrix* src, const tc_matrix* dst) {
+    const RowArgs a{src->d_data, dst->d_data, dst->d_scale, src->ld, dst->ld, src->rows, src->cols};
+    return wide(src) && wide(dst) ? encode_rows<T, true>(ctx, a) : encode_rows<T, false>(ctx, a);
+}
+template <class T>
+int run_decode(tc_ctx* ctx, const tc_matrix* src, const tc_matrix* dst) {
+    const RowArgs a{src->d_data, dst->d_data, src->d_scale, src->ld, dst->ld, src->rows, src->cols};
+    const uint64_t grid = (uint64_t)a.rows * ((a.cols + 2047) / 2048);
+    if (grid > 0x7FFFFFFFu) REFUSE(TC_ERR_SHAPE, "matrix too large");
+    if (wide(src) && wide(dst)) LAUNCH((checkpoint_decode<T, true>), dim3((uint32_t)grid), 256, 0, a);
+    else LAUNCH((checkpoint_decode<T, false>), dim3((uint32_t)grid), 256, 0, a);
+    return TC_OK;
+}
+template <class T>
+int run_norm(tc_ctx* ctx, int kind, const tc_matrix* x, const void* gamma, const void* beta, float eps, const tc_matrix* y, float* mean, float* rstd) {
+    const NormArgs a{x->d_data, x->dtype == TC_I8 ? x->d_scale : nullptr, gamma, beta, y->d_data, mean, rstd, x->ld, y->ld, x->rows, x->cols, eps, kind == TC_NORM_LAYER};
+    const bool w = wide(x) && wide(y) && (((uintptr_t)gamma | (uintptr_t)beta) & 15u) == 0;
+    return w ? norm_rows<T, true>(ctx, a) : norm_rows<T, false>(ctx, a);
+}
+template <class T>
+int run_norm_backward(tc_ctx* ctx, int kind, const tc_matrix* dy, const tc_matrix* x, const void* gamma, const float* mean, const float* rstd,
+                      const tc_matrix* dx, float* dgamma, float* dbeta, void* ws) {
+    const uint32_t groups = norm_back_groups(dy->rows, dy->cols);
+    float* part = dgamma || dbeta ? (float*)ws : nullptr;
+    const NormBackArgs a{dy->d_data, x->d_data, x->dtype == TC_I8 ? x->d_scale : nullptr, gamma, mean, rstd, dx ? dx->d_data : nullptr, part,
+                         dy->ld, x->ld, dx ? dx->ld : 0, dy->rows, dy->cols, kind == TC_NORM_LAYER};
+    const bool w = wide(dy) && wide(x) && (!dx || wide(dx)) && ((uintptr_t)gamma & 15u) == 0;
+    TRY((w ? norm_back_rows<T, true>(ctx, a, groups) : norm_back_rows<T, false>(ctx, a, groups)));
+    if (dgamma) TRY(sum_columns(ctx, part, 2 * (uint64_t)dy->cols, groups, dy->cols, dgamma));
+    if (dbeta) TRY(sum_columns(ctx, part + dy->cols, 2 * (uint64_t)dy->cols, groups, dy->cols, dbeta));
+    return TC_OK;
+}
+template <class T>
+int run_linear(tc_ctx* ctx, const tc_matrix* x, const tc_matrix* w, const void* bias, int act, const tc_matrix* residual, const tc_matrix* y, const tc_matrix* z) {
+    ProductArgs a = {};
+    a.p = Operand{w->d_data, w->ld};
+    a.q = Operand{x->d_data, x->ld};
+    a.np = w->rows;
+    a.nq = x->rows;
+    a.nr = w->cols;
+    a.out = y->d_data;
+    a.ldo = y->ld;
+    a.p_scale = w->dtype == TC_I8 ? w->d_scale : nullptr;
+    a.bias = bias;
+    if (residual) { a.residual = residual->d_data; a.ldres = residual->ld; }
+    if (z) { a.z = z->d_data; a.ldz = z->ld; }
+    a.act = act;
+    return a.p_scale ? multiply<T, true, true, true, false, true>(ctx, a) : multiply<T, true, false, true, false, true>(ctx, a);
+}
+template <class T>
+int run_linear_backward(tc_ctx* ctx, const tc_matrix* dy, const tc_matrix* x, const tc_matrix* w, int act, const tc_matrix* z, const tc_matrix* dz,
+                        const tc_matrix* dx, const tc_matrix* dw, float* dbias, void* ws) {
+    const uint32_t rows = dy->rows, out = dy->cols;
+    const BackPlan plan = back_plan(rows, out);
+    uint8_t* base = (uint8_t*)ws;
+    float* m = (float*)(base + plan.m);
+    const bool by_x = dw && x->dtype == TC_I8, by_w = dx && w->dtype == TC_I8;
+    if (by_x || by_w) {
+        hipLaunchKernelGGL(scale_peak, dim3(2), dim3(1024), 0, ctx_stream(ctx), by_x ? x->d_scale : nullptr, rows, by_w ? w->d_scale : nullptr, out, m);
+        int e = (int)hipGetLastError();
+        if (e) return ctx_fail_hip(ctx, e, "launch of scale_peak");
+    }
+    if (act != TC_ACT_NONE || by_x || by_w || dbias) {
+        SlopeArgs s = {};
+        s.dy = dy->d_data;
+        s.lddy = dy->ld;
+        bool wd = wide(dy);
+        if (act != TC_ACT_NONE) {
+            s.z = z->d_data;
+            s.z_scale = z->dtype == TC_I8 ? z->d_scale : nullptr;
+            s.ldz = z->ld;
+            s.dz = dz->d_data;
+            s.lddz = dz->ld;
+            wd = wd && wide(z) && wide(dz);
+        }
+        s.by_x = by_x ? base + plan.by_x : nullptr;
+        s.by_w = by_w ? base + plan.by_w : nullptr;
+        s.x_scale = by_x ? x->d_scale : nullptr;
+        s.w_scale = by_w ? w->d_scale : nullptr;
+        s.m = m;
+        s.part = dbias ? (float*)(base + plan.part) : nullptr;
+        s.ld_by = plan.ld_by;
+        s.rows = rows;
+        s.cols = out;
+        s.act = act;
+        const uint32_t groups = slope_groups(rows, out);
+        const dim3 grid((out + 511) / 512, groups);
+        if (wd) LAUNCH((slopes<T, true>), grid, 256, 0, s);
+        else LAUNCH((slopes<T, false>), grid, 256, 0, s);
+        if (dbias) TRY(sum_columns(ctx, s.part, out, groups, out, dbias));
+    }
+    const Operand plain = act == TC_ACT_NONE ? Operand{dy->d_data, dy->ld} : Operand{dz->d_data, dz->ld};
+    if (dx) {
+        ProductArgs a = {};
+        a.p = Operand{w->d_data, w->ld};
+        a.q = by_w ? Operand{base + plan.by_w, plan.ld_by} : plain;
+        a.np = w->cols;
+        a.nq = rows;
+        a.nr = out;
+        a.out = dx->d_data;
+        a.ldo = dx->ld;
+        a.factor = by_w ? m + 2 : nullptr;
+        TRY((by_w ? multiply<T, false, true, true, false, false>(ctx, a) : multiply<T, false, false, true, false, false>(ctx, a)));
+    }
+    if (dw) {
+        ProductArgs a = {};
+        a.p = Operand{x->d_data, x->ld};
+        a.q = by_x ? Operand{base + plan.by_x, plan.ld_by} : plain;
+        a.np = x->cols;
+        a.nq = out;
+        a.nr = rows;
+        a.out = dw->d_data;
+        a.ldo = dw->ld;
+        a.factor = by_x ? m : nullptr;
+        TRY((by_x ? multiply<T, false, true, false, false, false>(ctx, a) : multiply<T, false, false, false, false, false>(ctx, a)));
+    }
+    return TC_OK;
+}
+}  // namespace
+#endif
+
+#if defined(TC_HOST_EMU)
+#define RUN(name, dtype, ...) (emu::name(dtype, __VA_ARGS__), TC_OK)
+#else
+#define RUN(name, dtype, ...) ((dtype) == TC_F16 ? run_##name<_Float16>(ctx, __VA_ARGS__) : run_##name<__bf16>(ctx, __VA_ARGS__))
+#endif
+
+extern "C" int tc_checkpoint_encode(tc_ctx* ctx, const tc_matrix* src, const tc_matrix* dst) {
+    if (!ctx) return TC_ERR_ARG;
+    TRY(check_view(ctx, src, false));
+    TRY(check_view(ctx, dst, true));
+    if (dst->dtype != TC_I8) REFUSE(TC_ERR_ARG, "a checkpoint is int8");
+    TRY(check_shape(ctx, dst, src->rows, src->cols));
+    if (!src->rows) return TC_OK;
+    TRY(ctx_use_device(ctx));
+    return RUN(encode, src->dtype, src, dst);
+}
+extern "C" int tc_checkpoint_decode(tc_ctx* ctx, const tc_matrix* src, const tc_matrix* dst) {
+    if (!ctx) return TC_ERR_ARG;
+    TRY(check_view(ctx, src, true));
+    if (src->dtype != TC_I8) REFUSE(TC_ERR_ARG, "a checkpoint is int8");
+    TRY(check_view(ctx, dst, false));
+    TRY(check_shape(ctx, dst, src->rows, src->cols));
+    if (!src->rows) return TC_OK;
+    TRY(ctx_use_device(ctx));
+    return RUN(decode, dst->dtype, src, dst);
+}
+
+extern "C" int tc_norm(tc_ctx* ctx, int kind, const tc_matrix* x, const void* d_gamma, const void* d_beta, float eps, const tc_matrix* y,
+                       float* d_mean, float* d_rstd) {
+    if (!ctx) return TC_ERR_ARG;
+    if (kind != TC_NORM_LAYER && kind != TC_NORM_RMS) REFUSE(TC_ERR_ARG, "unknown norm");
+    if (!(eps > 0.0f && eps < 1.0f)) REFUSE(TC_ERR_ARG, "eps outside (0, 1)");
+    TRY(check_view(ctx, x, true));
+    TRY(check_view(ctx, y, false));
+    if (x->dtype != TC_I8) TRY(check_type(ctx, x, y->dtype));
+    TRY(check_shape(ctx, y, x->rows, x->cols));
+    if (x->cols > TC_NORM_MAX_COLS) REFUSE(TC_ERR_SHAPE, "rows longer than TC_NORM_MAX_COLS");
+    TRY(check_vector(ctx, d_gamma, 2));
+    TRY(check_vector(ctx, d_beta, 2));
+    TRY(check_vector(ctx, d_mean, 4));
+    TRY(check_vector(ctx, d_rstd, 4));
+    if (!x->rows) return TC_OK;
+    TRY(ctx_use_device(ctx));
+    return RUN(norm, y->dtype, kind, x, d_gamma, d_beta, eps, y, d_mean, d_rstd);
+}
+extern "C" int tc_norm_backward_workspace(uint32_t rows, uint32_t cols, size_t* bytes) {
+    if (!bytes) return TC_ERR_ARG;
+    if (rows > 0x7FFFFFFFu || cols == 0 || cols > TC_NORM_MAX_COLS) return TC_ERR_SHAPE;
+    *bytes = (size_t)norm_back_groups(rows, cols) * 2 * cols * 4;
+    return TC_OK;
+}
+extern "C" int tc_norm_backward(tc_ctx* ctx, int kind, const tc_matrix* dy, const tc_matrix* x, const void* d_gamma, const float* d_mean,
+                                const float* d_rstd, const tc_matrix* dx, float* d_dgamma, float* d_dbeta, void* d_workspace,
+                                size_t workspace_bytes) {
+    if (!ctx) return TC_ERR_ARG;
+    if (kind != TC_NORM_LAYER && kind != TC_NORM_RMS) REFUSE(TC_ERR_ARG, "unknown norm");
+    TRY(check_view(ctx, dy, false));
+    TRY(check_view(ctx, x, true));
+    if (x->dtype != TC_I8) TRY(check_type(ctx, x, dy->dtype));
+    TRY(check_shape(ctx, x, dy->rows, dy->cols));
+    if (dx) {
+        TRY(check_view(ctx, dx, false));
+        TRY(check_type(ctx, dx, dy->dtype));
+        TRY(check_shape(ctx, dx, dy->rows, dy->cols));
+    }
+    if (dy->cols > TC_NORM_MAX_COLS) REFUSE(TC_ERR_SHAPE, "rows longer than TC_NORM_MAX_COLS");
+    if (dy->rows && (!d_rstd || (kind == TC_NORM_LAYER && !d_mean))) REFUSE(TC_ERR_ARG, "statistics of the forward pass missing");
+    TRY(check_vector(ctx, d_gamma, 2));
+    TRY(check_vector(ctx, d_mean, 4));
+    TRY(check_vector(ctx, d_rstd, 4));
+    TRY(check_vector(ctx, d_dgamma, 4));
+    TRY(check_vector(ctx, d_dbeta, 4));
+    if (!dx && !d_dgamma && !d_dbeta) return TC_OK;
+    if (d_dgamma || d_dbeta) {
+        size_t need = 0;
+        TRY(tc_norm_backward_workspace(dy->rows, dy->cols, &need));
+        TRY(check_workspace(ctx, d_workspace, workspace_bytes, need));
+    }
+    TRY(ctx_use_device(ctx));
+    if (!dy->rows) {
+#if !defined(TC_HOST_EMU)
+        if (d_dgamma) TRY(clear_rows<float>(ctx, d_dgamma, dy->cols, 1, dy->cols));
+        if (d_dbeta) TRY(clear_rows<float>(ctx, d_dbeta, dy->cols, 1, dy->cols));
+        return TC_OK;
+#endif
+    }
+    return RUN(norm_backward, dy->dtype, kind, dy, x, d_gamma, d_mean, d_rstd, dx, d_dgamma, d_dbeta, d_workspace);
+}
+
+static bool linear_sizes(uint32_t rows, uint32_t in, uint32_t out) {
+    return rows <= 0x7FFFFFFFu && in >= 1 && in <= TC_LAYER_MAX_COLS && out >= 1 && out <= TC_LAYER_MAX_COLS;
+}
+extern "C" int tc_linear_workspace(uint32_t rows, uint32_t in, uint32_t out, size_t* bytes) {
+    if (!bytes) return TC_ERR_ARG;
+    if (!linear_sizes(rows, in, out)) return TC_ERR_SHAPE;
+    *bytes = 0;
+    return TC_OK;
+}
+extern "C" int tc_linear(tc_ctx* ctx, const tc_matrix* x, const tc_matrix* w, const void* d_bias, int activation, const tc_matrix* residual,
+                         const tc_matrix* y, const tc_matrix* z, void* d_workspace, size_t workspace_bytes) {
+    if (!ctx) return TC_ERR_ARG;
+    if (activation < TC_ACT_NONE || activation > TC_ACT_SILU) REFUSE(TC_ERR_ARG, "unknown activation");
+    TRY(check_view(ctx, x, false));
+    TRY(check_view(ctx, w, true));
+    if (!w->rows) REFUSE(TC_ERR_SHAPE, "weights without rows");
+    if (w->dtype != TC_I8) TRY(check_type(ctx, w, x->dtype));
+    if (w->cols != x->cols || w->rows > TC_LAYER_MAX_COLS) REFUSE(TC_ERR_SHAPE, "weights whose shape does not fit the input");
+    const tc_matrix* outs[3] = {y, residual, z};
+    for (int i = 0; i < 3; ++i) {
+        if (i && !outs[i]) continue;
+        TRY(check_view(ctx, outs[i], false));
+        TRY(check_type(ctx, outs[i], x->dtype));
+        TRY(check_shape(ctx, outs[i], x->rows, w->rows));
+    }
+    TRY(check_vector(ctx, d_bias, 2));
+    size_t need = 0;
+    TRY(tc_linear_workspace(x->rows, x->cols, w->rows, &need));
+    TRY(check_workspace(ctx, d_workspace, workspace_bytes, need));
+    if (!x->rows) return TC_OK;
+    TRY(ctx_use_device(ctx));
+    return RUN(linear, x->dtype, x, w, d_bias, activation, residual, y, z);
+}
+extern "C" int tc_linear_backward_workspace(uint32_t rows, uint32_t in, uint32_t out, size_t* bytes) {
+    if (!bytes) return TC_ERR_ARG;
+    if (!linear_sizes(rows, in, out)) return TC_ERR_SHAPE;
+    *bytes = back_plan(rows, out).bytes;
+    return TC_OK;
+}
+extern "C" int tc_linear_backward(tc_ctx* ctx, const tc_matrix* dy, const tc_matrix* x, const tc_matrix* w, int activation, const tc_matrix* z,
+                                  const tc_matrix* dz, const tc_matrix* dx, const tc_matrix* dw, float* d_dbias, void* d_workspace,
+                                  size_t workspace_bytes) {
+    if (!ctx) return TC_ERR_ARG;
+    if (activation < TC_ACT_NONE || activation > TC_ACT_SILU) REFUSE(TC_ERR_ARG, "unknown activation");
+    TRY(check_view(ctx, dy, false));
+    const uint32_t rows = dy->rows, out = dy->cols;
+    uint32_t in = 1;
+    if (activation == TC_ACT_NONE) {
+        if (z || dz) REFUSE(TC_ERR_ARG, "without an activation z and dz must be null");
+    } else {
+        TRY(check_view(ctx, z, true));
+        TRY(check_view(ctx, dz, false));
+        if (z->dtype != TC_I8) TRY(check_type(ctx, z, dy->dtype));
+        TRY(check_type(ctx, dz, dy->dtype));
+        TRY(check_shape(ctx, z, rows, out));
+        TRY(check_shape(ctx, dz, rows, out));
+    }
+    if (dx) {
+        TRY(check_view(ctx, dx, false));
+        TRY(check_type(ctx, dx, dy->dtype));
+        in = dx->cols;
+        TRY(check_shape(ctx, dx, rows, in));
+        TRY(check_view(ctx, w, true));
+        if (w->dtype != TC_I8) TRY(check_type(ctx, w, dy->dtype));
+        TRY(check_shape(ctx, w, out, in));
+    }
+    if (dw) {
+        TRY(check_view(ctx, dw, false));
+        TRY(check_type(ctx, dw, dy->dtype));
+        if (dx && dw->cols != in) REFUSE(TC_ERR_SHAPE, "matrices of shapes that do not fit together");
+        in = dw->cols;
+        TRY(check_shape(ctx, dw, out, in));
+        TRY(check_view(ctx, x, true));
+        if (x->dtype != TC_I8) TRY(check_type(ctx, x, dy->dtype));
+        TRY(check_shape(ctx, x, rows, in));
+    }
+    TRY(check_vector(ctx, d_dbias, 4));
+    size_t need = 0;
+    TRY(tc_linear_backward_workspace(rows, in, out, &need));
+    TRY(check_workspace(ctx, d_workspace, workspace_bytes, need));
+    TRY(ctx_use_device(ctx));
+    if (!rows) {
+#if !defined(TC_HOST_EMU)
+        if (dw) TRY(dw->dtype == TC_F16 ? clear_rows<_Float16>(ctx, dw->d_data, dw->ld, out, in) : clear_rows<__bf16>(ctx, dw->d_data, dw->ld, out, in));
+        if (d_dbias) TRY(clear_rows<float>(ctx, d_dbias, out, 1, out));
+        return TC_OK;
+#endif
+    }
+    return RUN(linear_backward, dy->dtype, dy, x, w, activation, z, dz, dx, dw, d_dbias, d_workspace);
+}

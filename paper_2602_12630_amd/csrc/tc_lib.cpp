@@ -16,6 +16,7 @@
 #include <vector>
 
 #include "../../include/tc.h"
+#include "ctx.h"
 #include "kernels.h"
 #include "pairing.h"
 #include "selector.h"
@@ -173,6 +174,16 @@ static int fail_hip(tc_ctx* ctx, int e, const char* where) {
         int rc_ = (call);         \
         if (rc_ != TC_OK) return rc_; \
     } while (0)
+
+namespace tc {
+rt::stream_t ctx_stream(const tc_ctx* ctx) { return ctx->stream; }
+int ctx_use_device(tc_ctx* ctx) {
+    RT(rt::set_device(ctx->device));
+    return TC_OK;
+}
+int ctx_fail(tc_ctx* ctx, int code, const char* msg) { return fail(ctx, code, msg); }
+int ctx_fail_hip(tc_ctx* ctx, int e, const char* where) { return fail_hip(ctx, e, where); }
+}  // namespace tc
 
 static size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
