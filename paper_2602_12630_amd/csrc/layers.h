@@ -169,34 +169,36 @@ template <class T, bool WIDE, int TH, int NCH>
 __global__ __launch_bounds__(TH < 256 ? 256 : TH) void checkpoint_encode(const RowArgs a) {
     __shared__ float cells[16];
     const int t = threadIdx.x % TH;
-    const uint32_t row = blockIdx.x * (TH < 256 ? 256 / TH : 1) + threadIdx.x / TH;
-    if (row >= a.rows) return;                       /* whole waves, and only where no barrier follows */
-    const T* src = (const T*)a.src + row * a.ld_src;
-    int8_t* dst = (int8_t*)a.dst + row * a.ld_dst;
+    constexpr uint32_t SETS = TH < 256 ? 256 / TH : 1;
     const int chunks = NCH ? NCH : (a.cols + TH * 8 - 1) / (TH * 8);
-    float x[NCH ? NCH : 1][8];
-    float m = 0.0f;
-    for (int c = 0; c < chunks; ++c) {
-        float* v = x[NCH ? c : 0];
-        load8<T, TH, WIDE>(src, t, c, a.cols, v);
-        for (int j = 0; j < 8; ++j) m = fmaxf(m, finite_magnitude(v[j]));
-    }
-    m = group_max<TH>(m, cells, t);
-    if (t == 0) a.scale[row] = m / 127.0f;
-    const int e = m > 0.0f ? -ilogbf(m) : 0;
-    const float amax = m > 0.0f ? ldexpf(m, e) : 1.0f, inv = 1.0f / amax;
-    for (int c = 0; c < chunks; ++c) {
-        float* v = x[NCH ? c : 0];
-        if (!NCH) load8<T, TH, WIDE>(src, t, c, a.cols, v);
-        if (WIDE) {
-            const uint32_t k = row_col<TH, true>(t, c, 0);
-            q8 q;
-            for (int j = 0; j < 8; ++j) q[j] = (int8_t)quantised(v[j], amax, inv, e);
-            if (k < a.cols) *(q8*)(dst + k) = q;
-        } else {
-            for (int j = 0; j < 8; ++j) {
-                const uint32_t k = row_col<TH, false>(t, c, j);
-                if (k < a.cols) dst[k] = (int8_t)quantised(v[j], amax, inv, e);
+    /* where waves share a row, all of them run the same rounds; where they do not, there is no barrier */
+    for (uint64_t row = (uint64_t)blockIdx.x * SETS + threadIdx.x / TH; row < a.rows; row += (uint64_t)gridDim.x * SETS) {
+        const T* src = (const T*)a.src + row * a.ld_src;
+        int8_t* dst = (int8_t*)a.dst + row * a.ld_dst;
+        float x[NCH ? NCH : 1][8];
+        float m = 0.0f;
+        for (int c = 0; c < chunks; ++c) {
+            float* v = x[NCH ? c : 0];
+            load8<T, TH, WIDE>(src, t, c, a.cols, v);
+            for (int j = 0; j < 8; ++j) m = fmaxf(m, finite_magnitude(v[j]));
+        }
+        m = group_max<TH>(m, cells, t);
+        if (t == 0) a.scale[row] = m / 127.0f;
+        const int e = m > 0.0f ? -ilogbf(m) : 0;
+        const float amax = m > 0.0f ? ldexpf(m, e) : 1.0f, inv = 1.0f / amax;
+        for (int c = 0; c < chunks; ++c) {
+            float* v = x[NCH ? c : 0];
+            if (!NCH) load8<T, TH, WIDE>(src, t, c, a.cols, v);
+            if (WIDE) {
+                const uint32_t k = row_col<TH, true>(t, c, 0);
+                q8 q;
+                for (int j = 0; j < 8; ++j) q[j] = (int8_t)quantised(v[j], amax, inv, e);
+                if (k < a.cols) *(q8*)(dst + k) = q;
+            } else {
+                for (int j = 0; j < 8; ++j) {
+                    const uint32_t k = row_col<TH, false>(t, c, j);
+                    if (k < a.cols) dst[k] = (int8_t)quantised(v[j], amax, inv, e);
+                }
             }
         }
     }
@@ -204,12 +206,11 @@ __global__ __launch_bounds__(TH < 256 ? 256 : TH) void checkpoint_encode(const R
 /* 256 lanes take 2048 entries of a row */
 template <class T, bool WIDE>
 __global__ __launch_bounds__(256) void checkpoint_decode(const RowArgs a) {
-    const uint32_t per_row = (a.cols + 2047) / 2048;
-    const uint32_t row = blockIdx.x / per_row;
-    const int c = blockIdx.x % per_row;
-    float v[8];
-    load8q<256, WIDE>((const int8_t*)a.src + row * a.ld_src, a.scale[row], threadIdx.x, c, a.cols, v);
-    store8<T, 256, WIDE>((T*)a.dst + row * a.ld_dst, threadIdx.x, c, a.cols, v);
+    for (uint64_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
+        float v[8];
+        load8q<256, WIDE>((const int8_t*)a.src + row * a.ld_src, a.scale[row], threadIdx.x, blockIdx.x, a.cols, v);
+        store8<T, 256, WIDE>((T*)a.dst + row * a.ld_dst, threadIdx.x, blockIdx.x, a.cols, v);
+    }
 }
 
 /* ---- norms --------------------------------------------------------------------------------------------
@@ -229,44 +230,45 @@ template <class T, bool WIDE, int TH, int NCH>
 __global__ __launch_bounds__(TH < 256 ? 256 : TH) void norm_forward(const NormArgs a) {
     __shared__ float cells[16];
     const int t = threadIdx.x % TH;
-    const uint32_t row = blockIdx.x * (TH < 256 ? 256 / TH : 1) + threadIdx.x / TH;
-    if (row >= a.rows) return;
-    float x[NCH][8];
-    for (int c = 0; c < NCH; ++c) {
-        if (a.scale) load8q<TH, WIDE>((const int8_t*)a.x + row * a.ldx, a.scale[row], t, c, a.cols, x[c]);
-        else load8<T, TH, WIDE>((const T*)a.x + row * a.ldx, t, c, a.cols, x[c]);
-    }
-    const float per = 1.0f / (float)a.cols;
-    float mean = 0.0f;
-    if (a.centred) {
+    constexpr uint32_t SETS = TH < 256 ? 256 / TH : 1;
+    for (uint64_t row = (uint64_t)blockIdx.x * SETS + threadIdx.x / TH; row < a.rows; row += (uint64_t)gridDim.x * SETS) {
+        float x[NCH][8];
+        for (int c = 0; c < NCH; ++c) {
+            if (a.scale) load8q<TH, WIDE>((const int8_t*)a.x + row * a.ldx, a.scale[row], t, c, a.cols, x[c]);
+            else load8<T, TH, WIDE>((const T*)a.x + row * a.ldx, t, c, a.cols, x[c]);
+        }
+        const float per = 1.0f / (float)a.cols;
+        float mean = 0.0f;
+        if (a.centred) {
+            float s = 0.0f;
+            for (int c = 0; c < NCH; ++c)
+                for (int j = 0; j < 8; ++j) s += x[c][j];
+            mean = group_sum<TH>(s, cells, t) * per;
+        }
         float s = 0.0f;
         for (int c = 0; c < NCH; ++c)
-            for (int j = 0; j < 8; ++j) s += x[c][j];
-        mean = group_sum<TH>(s, cells, t) * per;
-    }
-    float s = 0.0f;
-    for (int c = 0; c < NCH; ++c)
-        for (int j = 0; j < 8; ++j) {
-            const float d = row_col<TH, WIDE>(t, c, j) < a.cols ? x[c][j] - mean : 0.0f;
-            x[c][j] = d;
-            s += d * d;
+            for (int j = 0; j < 8; ++j) {
+                const float d = row_col<TH, WIDE>(t, c, j) < a.cols ? x[c][j] - mean : 0.0f;
+                x[c][j] = d;
+                s += d * d;
+            }
+        const float rstd = 1.0f / sqrtf(group_sum<TH>(s, cells, t) * per + a.eps);
+        if (t == 0) {
+            if (a.mean) a.mean[row] = mean;
+            if (a.rstd) a.rstd[row] = rstd;
         }
-    const float rstd = 1.0f / sqrtf(group_sum<TH>(s, cells, t) * per + a.eps);
-    if (t == 0) {
-        if (a.mean) a.mean[row] = mean;
-        if (a.rstd) a.rstd[row] = rstd;
-    }
-    for (int c = 0; c < NCH; ++c) {
-        float g[8], b[8];
-        if (a.gamma) load8<T, TH, WIDE>((const T*)a.gamma, t, c, a.cols, g);
-        if (a.beta) load8<T, TH, WIDE>((const T*)a.beta, t, c, a.cols, b);
-        for (int j = 0; j < 8; ++j) {
-            float v = x[c][j] * rstd;
-            if (a.gamma) v *= g[j];
-            if (a.beta) v += b[j];
-            x[c][j] = v;
+        for (int c = 0; c < NCH; ++c) {
+            float g[8], b[8];
+            if (a.gamma) load8<T, TH, WIDE>((const T*)a.gamma, t, c, a.cols, g);
+            if (a.beta) load8<T, TH, WIDE>((const T*)a.beta, t, c, a.cols, b);
+            for (int j = 0; j < 8; ++j) {
+                float v = x[c][j] * rstd;
+                if (a.gamma) v *= g[j];
+                if (a.beta) v += b[j];
+                x[c][j] = v;
+            }
+            store8<T, TH, WIDE>((T*)a.y + row * a.ldy, t, c, a.cols, x[c]);
         }
-        store8<T, TH, WIDE>((T*)a.y + row * a.ldy, t, c, a.cols, x[c]);
     }
 }
 
@@ -379,8 +381,8 @@ __global__ __launch_bounds__(1024) void column_sums(const ColumnSumArgs a) {
  *     dx = dz w     p: inputs,  q: rows,    r: outputs  P = w   r across memory   Q = dz  r along memory
  *     dw = dz^T x   p: inputs,  q: outputs, r: rows     P = x   r across memory   Q = dz  r across memory
  * P is the first operand of the matrix instruction and Q the second, so that a lane ends up with four neighbouring
- * entries of a row of out.  Tiles lie in LDS as they lie in memory: where r runs along memory, rows of 64 r in 16-byte pieces, piece k
- * of row i in place k ^ (i & 7); where it runs across, rows of the tile's p in 32-byte pieces, piece k of row r in place k ^ f(r), read through the transposing
+ * entries of a row of out.  Tiles lie in LDS as they lie in memory: where r runs along memory, rows of BK r in 16-byte pieces, piece k
+ * of row i in place k ^ turn(i); where it runs across, rows of the tile's p in 32-byte pieces, piece k of row r in place k ^ f(r), read through the transposing
  * LDS load.  With both rules the sixteen rows that a wave reads at once fall on all banks. */
 struct Operand {
     const void* d;
@@ -400,6 +402,10 @@ struct ProductArgs {
     uint64_t ldz;
     const float* factor;             /* gradients: everything times this number; null: 1 */
     int act;
+    float* part;                     /* [split][nq][ldp] unfinished sums, where r is split; null: the whole of r in one go */
+    uint64_t ldp;
+    uint32_t r_split;                /* r of one split */
+    int wide_out;                    /* every row of the epilogue's tensors can be accessed in pieces of eight */
 };
 template <class T> __device__ __forceinline__ f4 mfma(typename Vec<T>::v8 a, typename Vec<T>::v8 b, f4 c);
 template <> __device__ __forceinline__ f4 mfma<_Float16>(Vec<_Float16>::v8 a, Vec<_Float16>::v8 b, f4 c) {
@@ -409,18 +415,17 @@ template <> __device__ __forceinline__ f4 mfma<__bf16>(Vec<__bf16>::v8 a, Vec<__
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 
-static const int BK = 64;            /* r per step */
-
-/* A tile of an operand: SIDE of p (or q) by BK of r */
-template <class T, bool ALONG, bool EIGHT, int SIDE>
+/* A tile of an operand: SIDE of p (or q) by BK of r, 32 or 64 */
+template <class T, bool ALONG, bool EIGHT, int SIDE, int BK>
 struct Tile {
     typedef typename Vec<T>::v8 v8;
     typedef short s4 __attribute__((ext_vector_type(4)));
     static constexpr int ELEMENTS = SIDE * BK;
     __device__ static __forceinline__ int spread(int r) { return SIDE >= 128 ? (r & 3) | ((r >> 3) & 1) << 2 : r & 3; }
+    __device__ static __forceinline__ int turn(int line) { return BK == 64 ? line & 7 : (line >> 1) & 3; }
     /* where the eight elements number `piece` of line `line` lie: line = p of r pieces, or r of p pieces */
     __device__ static __forceinline__ int place(int line, int piece) {
-        if (ALONG) return line * BK + ((piece ^ (line & 7)) << 3);
+        if (ALONG) return line * BK + ((piece ^ turn(line)) << 3);
         return line * SIDE + ((((piece >> 1) ^ spread(line)) << 1 | (piece & 1)) << 3);
     }
     /* eight elements along memory: (line, col .. col + 7) of an operand of lines x cols; outside: zeros */
@@ -457,63 +462,110 @@ struct Tile {
     }
 };
 
-/* four neighbouring entries of a row of out, from column p on */
+/* eight neighbouring entries of a row of out, from column p on; whole: they are all there and lie on 16 bytes */
 template <class T>
-__device__ __forceinline__ void put4(void* base, uint64_t ld, uint32_t q, uint32_t p, uint32_t np, const float* v) {
+__device__ __forceinline__ void put8(void* base, uint64_t ld, uint32_t q, uint32_t p, uint32_t np, bool whole, const float* v) {
     T* at = (T*)base + q * ld + p;
-    if (p + 4 <= np && ((uintptr_t)at & 7u) == 0) {
-        typename Vec<T>::v4 x;
-        for (int i = 0; i < 4; ++i) x[i] = (T)v[i];
-        *(typename Vec<T>::v4*)at = x;
+    if (whole) {
+        typename Vec<T>::v8 x;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = (T)v[i];
+        *(typename Vec<T>::v8*)at = x;
     } else {
-        for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
             if (p + i < np) at[i] = (T)v[i];
     }
 }
 template <class T>
-__device__ __forceinline__ void get4(const void* base, uint64_t ld, uint32_t q, uint32_t p, uint32_t np, float* v) {
+__device__ __forceinline__ void get8(const void* base, uint64_t ld, uint32_t q, uint32_t p, uint32_t np, bool whole, float* v) {
     const T* at = (const T*)base + q * ld + p;
-    if (p + 4 <= np && ((uintptr_t)at & 7u) == 0) {
-        const typename Vec<T>::v4 x = *(const typename Vec<T>::v4*)at;
-        for (int i = 0; i < 4; ++i) v[i] = (float)x[i];
+    if (whole) {
+        const typename Vec<T>::v8 x = *(const typename Vec<T>::v8*)at;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = (float)x[i];
     } else {
-        for (int i = 0; i < 4; ++i) v[i] = p + i < np ? (float)at[i] : 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = p + i < np ? (float)at[i] : 0.0f;
     }
 }
 template <class T, bool FORWARD>
-__device__ __forceinline__ void finish4(const ProductArgs& a, uint32_t q, uint32_t p, float* v) {
+__device__ __forceinline__ void finish8(const ProductArgs& a, uint32_t q, uint32_t p, float* v) {
     if (q >= a.nq || p >= a.np) return;
+    const bool whole = a.wide_out;
     if (FORWARD) {
-        for (int i = 0; i < 4; ++i) {
-            if (p + i >= a.np) continue;
-            if (a.p_scale) v[i] *= a.p_scale[p + i];
-            if (a.bias) v[i] += (float)((const T*)a.bias)[p + i];
+        float r[8];
+        if (a.p_scale) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] *= p + i < a.np ? a.p_scale[p + i] : 0.0f;
         }
-        if (a.z) put4<T>(a.z, a.ldz, q, p, a.np, v);
-        for (int i = 0; i < 4; ++i) v[i] = activate(v[i], a.act);
+        if (a.bias) {
+            get8<T>(a.bias, 0, 0, p, a.np, whole, r);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] += r[i];
+        }
+        if (a.z) put8<T>(a.z, a.ldz, q, p, a.np, whole, v);
+        if (a.act != TC_ACT_NONE) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = activate(v[i], a.act);
+        }
         if (a.residual) {
-            float r[4];
-            get4<T>(a.residual, a.ldres, q, p, a.np, r);
-            for (int i = 0; i < 4; ++i) v[i] += r[i];
+            get8<T>(a.residual, a.ldres, q, p, a.np, whole, r);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] += r[i];
         }
     } else if (a.factor) {
         const float f = a.factor[0];
-        for (int i = 0; i < 4; ++i) v[i] *= f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] *= f;
     }
-    put4<T>(a.out, a.ldo, q, p, a.np, v);
+    put8<T>(a.out, a.ldo, q, p, a.np, whole, v);
+}
+/* A wave's NP x NQ blocks of sixteen by sixteen, through a piece of LDS of its own (NP * 16 + 4 floats for each of sixteen q): a lane of
+ * the matrix instruction holds four entries of a row, and memory wants whole lines.  The workgroup must have passed a barrier since
+ * LDS was last read otherwise. */
+template <int NP> constexpr int drain_bytes() { return 16 * (NP * 16 + 4) * 4; }
+template <class T, bool FORWARD, int NP, int NQ>
+__device__ __forceinline__ void drain(const ProductArgs& a, f4 (&acc)[NP][NQ], uint8_t* lds, uint32_t q0, uint32_t p0, uint32_t split, int lane) {
+    float* buf = (float*)lds;
+    constexpr int LD = NP * 16 + 4, GROUPS = NP * 2, ROWS = 64 / GROUPS;
+#pragma unroll
+    for (int j = 0; j < NQ; ++j) {
+#pragma unroll
+        for (int i = 0; i < NP; ++i) *(f4*)(buf + (lane & 15) * LD + i * 16 + (lane >> 4) * 4) = acc[i][j];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");        /* lanes read what others of the wave have written */
+#pragma unroll 1
+        for (int r = lane / GROUPS; r < 16; r += ROWS) {
+            const float* at = buf + r * LD + (lane % GROUPS) * 8;
+            const f4 lo = *(const f4*)at, hi = *(const f4*)(at + 4);
+            const uint32_t q = q0 + j * 16 + r, p = p0 + (lane % GROUPS) * 8;
+            if (a.part) {
+                if (q < a.nq && p < a.np) {
+                    f4* to = (f4*)(a.part + (split * (uint64_t)a.nq + q) * a.ldp + p);
+                    to[0] = lo;
+                    to[1] = hi;
+                }
+            } else {
+                float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+                finish8<T, FORWARD>(a, q, p, v);
+            }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
 }
 
-template <class T, bool P_ALONG, bool P_EIGHT, bool Q_ALONG, bool Q_EIGHT, bool FORWARD>
+template <class T, bool P_ALONG, bool P_EIGHT, bool Q_ALONG, bool FORWARD>
 __global__ __launch_bounds__(256) void product(const ProductArgs a) {
-    constexpr int SP = 128, SQ = 128;
-    typedef Tile<T, P_ALONG, P_EIGHT, SP> TP;
-    typedef Tile<T, Q_ALONG, Q_EIGHT, SQ> TQ;
-    __shared__ __align__(16) T lp[TP::ELEMENTS];
-    __shared__ __align__(16) T lq[TQ::ELEMENTS];
+    constexpr int SP = 128, SQ = 128, BK = 64;
+    typedef Tile<T, P_ALONG, P_EIGHT, SP, BK> TP;
+    typedef Tile<T, Q_ALONG, false, SQ, BK> TQ;
+    __shared__ __align__(16) uint8_t lds[(TP::ELEMENTS + TQ::ELEMENTS) * sizeof(T)];
+    T *lp = (T*)lds, *lq = lp + TP::ELEMENTS;
     const uint32_t tiles_p = (a.np + SP - 1) / SP;
     const uint64_t p0 = (uint64_t)(blockIdx.x % tiles_p) * SP, q0 = (uint64_t)(blockIdx.x / tiles_p) * SQ;
     const int t = threadIdx.x, lane = t & 63, wp = (t >> 6) & 1, wq = t >> 7;
     f4 acc[4][4] = {};
+#pragma unroll 1
     for (uint32_t r0 = 0; r0 < a.nr; r0 += BK) {
         __syncthreads();
         TP::template fill<256>(lp, a.p, p0, a.np, r0, a.nr, t);
@@ -527,11 +579,312 @@ __global__ __launch_bounds__(256) void product(const ProductArgs a) {
                 for (int j = 0; j < 4; ++j) acc[i][j] = mfma<T>(fp[i], fq[j], acc[i][j]);
         }
     }
-    for (int i = 0; i < 4; ++i)
-        for (int j = 0; j < 4; ++j) {
-            float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
-            finish4<T, FORWARD>(a, (uint32_t)q0 + wq * 64 + j * 16 + (lane & 15), (uint32_t)p0 + wp * 64 + i * 16 + (lane >> 4) * 4, v);
+    __syncthreads();
+    drain<T, FORWARD, 4, 4>(a, acc, lds + (t >> 6) * drain_bytes<4>(), (uint32_t)q0 + wq * 64, (uint32_t)p0 + wp * 64, 0, lane);
+}
+
+/* ---- products of aligned operands --------------------------------------------------------------------------
+ * The same product where both operands can be read in 16-byte pieces (int8: 8-byte ones).  16-bit tiles go from memory to LDS without
+ * passing through registers.  That direct load writes the lanes' pieces side by side, so the places of a tile are dealt out
+ * on the memory side: place n takes the piece that belongs there.  Buffer addresses: a piece outside the operand gets an offset past the buffer's end and reads
+ * zeros.  int8 tiles pass through registers, where they become the other operand's type. */
+/* eight int8 in two words -> eight of T, exactly.  float16: a byte with its sign bit flipped is q + 128; put under the exponent of 1024 it reads 1152 + q. */
+template <class T> __device__ __forceinline__ typename Vec<T>::v8 widen(uint32_t lo, uint32_t hi);
+template <> __device__ __forceinline__ Vec<_Float16>::v8 widen<_Float16>(uint32_t lo, uint32_t hi) {
+    typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+    union {
+        h2 h[4];
+        Vec<_Float16>::v8 v;
+    } u;
+    lo ^= 0x80808080u;
+    hi ^= 0x80808080u;
+    const h2 bias = {(_Float16)1152.0f, (_Float16)1152.0f};
+    u.h[0] = __builtin_bit_cast(h2, __builtin_amdgcn_perm(0x64646464u, lo, 0x04010400u)) - bias;
+    u.h[1] = __builtin_bit_cast(h2, __builtin_amdgcn_perm(0x64646464u, lo, 0x04030402u)) - bias;
+    u.h[2] = __builtin_bit_cast(h2, __builtin_amdgcn_perm(0x64646464u, hi, 0x04010400u)) - bias;
+    u.h[3] = __builtin_bit_cast(h2, __builtin_amdgcn_perm(0x64646464u, hi, 0x04030402u)) - bias;
+    return u.v;
+}
+template <> __device__ __forceinline__ Vec<__bf16>::v8 widen<__bf16>(uint32_t lo, uint32_t hi) {
+    union {
+        uint32_t w[4];
+        Vec<__bf16>::v8 v;
+    } u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int w = (int)(i < 2 ? lo : hi), at = i & 1 ? 16 : 0;
+        const float even = (float)(w << (24 - at) >> 24), odd = (float)(w << (16 - at) >> 24);
+        u.w[i] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, odd), __builtin_bit_cast(uint32_t, even), 0x07060302u);      /* the upper halves: a whole number under 256 has no more */
+    }
+    return u.v;
+}
+template <class T, bool ALONG, bool EIGHT, int SIDE, int TH, int BK>
+struct Feed {
+    typedef Tile<T, ALONG, EIGHT, SIDE, BK> tile;
+    typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+    static constexpr int N = SIDE * BK / 8 / TH, PIECES = ALONG ? BK / 8 : SIDE / 8, SIZE = EIGHT ? 1 : 2;
+    static constexpr uint32_t NOWHERE = 0x80000000u;
+    typedef u2 Held[EIGHT ? N : 1];
+    uint32_t off[N];
+    const char* base;
+    uint64_t step;
+    uint32_t nr, line_bytes;
+    __device__ static __forceinline__ int piece_of(int n) {
+        const int line = n / PIECES, slot = n % PIECES;
+        return ALONG ? slot ^ tile::turn(line) : ((slot >> 1) ^ tile::spread(line)) << 1 | (slot & 1);
+    }
+    /* r from `r0` on, `nr_` of them */
+    __device__ __forceinline__ void init(const Operand& o, uint64_t side0, uint32_t sides, uint32_t r0, uint32_t nr_, int t) {
+        nr = nr_;
+        line_bytes = (uint32_t)(o.ld * SIZE);
+        base = (const char*)o.d + (ALONG ? side0 * o.ld + r0 : r0 * o.ld + side0) * SIZE;
+        step = ALONG ? BK * SIZE : BK * o.ld * SIZE;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int n = i * TH + t, line = n / PIECES, piece = piece_of(n);
+            const bool in = side0 + (ALONG ? line : piece * 8) < sides;
+            off[i] = in ? line * line_bytes + piece * 8 * SIZE : NOWHERE;
         }
+    }
+    /* tile number k, to its place in LDS or into `held`; past the last one: zeros */
+    __device__ __forceinline__ void issue(T* lds, Held& held, uint32_t k, int t) {
+        const uint32_t rest = __builtin_amdgcn_readfirstlane(nr > k * BK ? nr - k * BK : 0);      /* a saturating difference, which is a vector instruction */
+        const char* at = base + (rest ? k * step : 0);
+        const uint32_t span = ALONG ? NOWHERE - 1 : (rest < BK ? rest : BK) * line_bytes;
+        const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)at, 0, span, 0x00020000);
+        if (ALONG && rest < BK) {        /* the last tile of r: pieces past its end go, for good */
+            asm volatile("");            /* a branch, not eight selections in every step */
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if ((uint32_t)piece_of(i * TH + t) * 8 >= rest) off[i] = NOWHERE;
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            uint32_t o = off[i];
+            if (EIGHT) held[i] = __builtin_amdgcn_raw_buffer_load_b64(r, o, 0, 0);
+            else
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(lds + (i * TH + (t & ~63)) * 8), 16, o, 0, 0, 0);
+        }
+    }
+    __device__ __forceinline__ void settle(T* lds, Held& held, int t) {
+        if (!EIGHT) return;
+#pragma unroll
+        for (int i = 0; i < N; ++i) *(typename Vec<T>::v8*)(lds + (i * TH + t) * 8) = widen<T>(held[i][0], held[i][1]);
+    }
+};
+/* Workgroups go to the eight XCDs in turn, each with an L2 of its own: an XCD takes neighbouring tiles, in blocks of four along q */
+__device__ __forceinline__ void tile_of(uint32_t b, uint32_t tiles_p, uint32_t tiles_q, uint32_t& tp, uint32_t& tq) {
+    const uint32_t n = tiles_p * tiles_q, per = n / 8, more = n % 8, x = b % 8;
+    const uint32_t i = x * per + (x < more ? x : more) + b / 8;
+    const uint32_t DEEP = 4;
+    const uint32_t band = i / (DEEP * tiles_p), first = band * DEEP, deep = tiles_q - first < DEEP ? tiles_q - first : DEEP;
+    const uint32_t j = i - band * DEEP * tiles_p;
+    /* the division runs in vector registers; buffer descriptors want scalar ones */
+    tq = __builtin_amdgcn_readfirstlane(first + j % deep);
+    tp = __builtin_amdgcn_readfirstlane(j / deep);
+}
+/* What both kernels below start with: the tile of this workgroup and its part of r */
+#define TC_PRODUCT_PROLOGUE                                                                                                 \
+    constexpr int TH = WP * WQ * 64, NP = SP / WP / 16, NQ = SQ / WQ / 16, STAGE = (SP + SQ) * BK;                          \
+    typedef Feed<T, P_ALONG, P_EIGHT, SP, TH, BK> FP;                                                                       \
+    typedef Feed<T, Q_ALONG, false, SQ, TH, BK> FQ;                                                                         \
+    extern __shared__ __align__(16) uint8_t lds_bytes[];                                                                    \
+    T* const lds = (T*)lds_bytes;                                                                                           \
+    const uint32_t tiles_p = (a.np + SP - 1) / SP, tiles_q = (a.nq + SQ - 1) / SQ;                                          \
+    const uint32_t split = __builtin_amdgcn_readfirstlane(blockIdx.x / (tiles_p * tiles_q)), r0 = split * a.r_split;                                        \
+    const uint32_t nr = a.nr - r0 < a.r_split ? a.nr - r0 : a.r_split, steps = (nr + BK - 1) / BK;                          \
+    uint32_t tp, tq;                                                                                                        \
+    tile_of(blockIdx.x % (tiles_p * tiles_q), tiles_p, tiles_q, tp, tq);                                                    \
+    const uint64_t p0 = (uint64_t)tp * SP, q0 = (uint64_t)tq * SQ;                                                          \
+    const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6), wp = w % WP, wq = w / WP;         \
+    FP fp;                                                                                                                  \
+    FQ fq;                                                                                                                  \
+    fp.init(a.p, p0, a.np, r0, nr, t);                                                                                      \
+    fq.init(a.q, q0, a.nq, r0, nr, t);                                                                                      \
+    f4 acc[NP][NQ] = {};
+#define TC_WAIT_AND_MEET(n) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(n) : "memory")
+#define TC_PRODUCT_EPILOGUE                                                                                                 \
+    TC_WAIT_AND_MEET(0);                                                                                                    \
+    drain<T, FORWARD, NP, NQ>(a, acc, lds_bytes + w * drain_bytes<NP>(), (uint32_t)q0 + wq * (SQ / WQ), (uint32_t)p0 + wp * (SP / WP), split, lane);
+
+/* Two stages of 64 r: one is multiplied while the other is filled; the two or more workgroups that share a compute unit cover each other's waits. */
+template <class T, bool P_ALONG, bool P_EIGHT, bool Q_ALONG, bool FORWARD, int SP, int SQ, int WP, int WQ>
+__global__ __launch_bounds__(WP * WQ * 64) void product_paired(const ProductArgs a) {
+    constexpr int BK = 64;
+    TC_PRODUCT_PROLOGUE
+    typename FP::Held hp;
+    typename FQ::Held hq;
+    fp.issue(lds, hp, 0, t);
+    fq.issue(lds + SP * BK, hq, 0, t);
+    fp.settle(lds, hp, t);
+#pragma unroll 1
+    for (uint32_t k = 0; k < steps; ++k) {
+        T* now = lds + (k & 1) * STAGE;
+        T* next = lds + (~k & 1) * STAGE;
+        TC_WAIT_AND_MEET(0);
+        fp.issue(next, hp, k + 1, t);
+        fq.issue(next + SP * BK, hq, k + 1, t);
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            typename Vec<T>::v8 x[NP], y[NQ];
+#pragma unroll
+            for (int j = 0; j < NQ; ++j) y[j] = FQ::tile::fragment(now + SP * BK, wq * (SQ / WQ) + j * 16, s, lane);
+#pragma unroll
+            for (int i = 0; i < NP; ++i) x[i] = FP::tile::fragment(now, wp * (SP / WP) + i * 16, s, lane);
+#pragma unroll
+            for (int i = 0; i < NP; ++i)
+#pragma unroll
+                for (int j = 0; j < NQ; ++j) acc[i][j] = mfma<T>(x[i], y[j], acc[i][j]);
+        }
+        fp.settle(next, hp, t);
+    }
+    TC_PRODUCT_EPILOGUE
+}
+
+/* Five stages of 32 r in all 160 KB of LDS, for tiles of 256 x 256, one workgroup to a compute unit.  While a stage is multiplied from registers, the next
+ * one is read into the other set of registers and the loads of the three after that are under way: at a step's barrier
+ * every wave has read the stage it multiplies and the next one has arrived (the loads of the two behind it may be
+ * outstanding).  Loads past the last stage bring zeros, so that the loop has no branches and the count of outstanding loads is always the same.
+ * 16-bit operands only: an int8 one of a product this large is widened beforehand, which costs less than its passage through registers. */
+template <class T, bool P_ALONG, bool Q_ALONG, bool FORWARD, int SP, int SQ, int WP, int WQ>
+__global__ __launch_bounds__(WP * WQ * 64) __attribute__((amdgpu_waves_per_eu(WP * WQ / 4, WP * WQ / 4))) void product_deep(const ProductArgs a) {
+    constexpr int BK = 32, STAGES = 5;
+    constexpr bool P_EIGHT = false;
+    TC_PRODUCT_PROLOGUE
+    constexpr int LOADS = FP::N + FQ::N;
+    typename FP::Held hp;
+    typename FQ::Held hq;
+    typename Vec<T>::v8 x0[NP], y0[NQ], x1[NP], y1[NQ];
+#define TC_READ(X, Y, place)                                                                                                            \
+    _Pragma("unroll") for (int j = 0; j < NQ; ++j) Y[j] = FQ::tile::fragment(lds + (place) * STAGE + SP * BK, wq * (SQ / WQ) + j * 16, 0, lane); \
+    _Pragma("unroll") for (int i = 0; i < NP; ++i) X[i] = FP::tile::fragment(lds + (place) * STAGE, wp * (SP / WP) + i * 16, 0, lane);
+#define TC_ORDER                                                                                                                        \
+    if (P_ALONG && Q_ALONG) {                                                                                                           \
+        __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);                                                                              \
+        _Pragma("unroll") for (int i = 0; i < NP + NQ; ++i) {                                                                           \
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);                                                                                   \
+            __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);                                                                          \
+        }                                                                                                                               \
+    }
+#define TC_STEP(k, X, Y, X2, Y2)                                                                                                        \
+    TC_WAIT_AND_MEET(LOADS * (STAGES - 3));                                                                                             \
+    fp.issue(lds + put * STAGE, hp, (k) + STAGES - 1, t);                                                                                \
+    fq.issue(lds + put * STAGE + SP * BK, hq, (k) + STAGES - 1, t);                                                                     \
+    TC_READ(X2, Y2, next)                                                                                                               \
+    _Pragma("unroll") for (int i = 0; i < NP; ++i)                                                                                      \
+        _Pragma("unroll") for (int j = 0; j < NQ; ++j) acc[i][j] = mfma<T>(X[i], Y[j], acc[i][j]);                                      \
+    TC_ORDER                                                                                                                            \
+    put = put + 1 == STAGES ? 0 : put + 1;                                                                                              \
+    next = next + 1 == STAGES ? 0 : next + 1;
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i) {
+        fp.issue(lds + i * STAGE, hp, i, t);
+        fq.issue(lds + i * STAGE + SP * BK, hq, i, t);
+    }
+    TC_WAIT_AND_MEET(LOADS * (STAGES - 2));
+    TC_READ(x0, y0, 0)
+    uint32_t next = 1, put = STAGES - 1;
+#pragma unroll 1
+    for (uint32_t k = 0; k < steps; k += 2) {
+        TC_STEP(k, x0, y0, x1, y1)
+        TC_STEP(k + 1, x1, y1, x0, y0)
+    }
+#undef TC_STEP
+#undef TC_ORDER
+#undef TC_READ
+    TC_PRODUCT_EPILOGUE
+}
+#undef TC_PRODUCT_PROLOGUE
+#undef TC_PRODUCT_EPILOGUE
+
+/* int8 rows -> the same whole numbers in T, side by side with a stride of ldo: 256 lanes take 2048 entries of a row */
+template <class T>
+__global__ __launch_bounds__(256) void widen_rows(const Operand o, T* out, uint64_t ldo, uint32_t rows, uint32_t cols) {
+    const uint32_t col = (blockIdx.x * 256 + threadIdx.x) * 8;
+    if (col >= cols) return;
+    for (uint64_t row = blockIdx.y; row < rows; row += gridDim.y) {
+        const uint2 q = *(const uint2*)((const int8_t*)o.d + row * o.ld + col);
+        *(typename Vec<T>::v8*)(out + row * ldo + col) = widen<T>(q.x, q.y);
+    }
+}
+
+/* the parts of a split product, added in order, and its epilogue: eight entries to a lane */
+template <class T, bool FORWARD>
+__global__ __launch_bounds__(256) void join_parts(const ProductArgs a, uint32_t splits) {
+    const uint32_t per = (a.np + 7) / 8;
+    const uint64_t n = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+    if (n >= (uint64_t)per * a.nq) return;
+    const uint32_t q = (uint32_t)(n / per), p = (uint32_t)(n % per) * 8;
+    f4 lo = {0, 0, 0, 0}, hi = {0, 0, 0, 0};
+    for (uint32_t i = 0; i < splits; ++i) {
+        const f4* at = (const f4*)(a.part + (i * (uint64_t)a.nq + q) * a.ldp + p);
+        lo += at[0];
+        hi += at[1];
+    }
+    float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    finish8<T, FORWARD>(a, q, p, v);
+}
+
+/* ---- a few rows -------------------------------------------------------------------------------------------------
+ * y = x w^T for at most sixteen rows of x: the weights are read once and that is all it costs.  A workgroup has sixteen of w's rows and its waves share r; each goes from memory
+ * straight into the matrix instruction: lane l takes 16 r of row l & 15, from 16 (l >> 4) on, the first eight of them for one
+ * instruction and the last eight for the next (any order of r does, if both operands have the same).  The waves' sums are added in order. */
+template <class T, bool EIGHT, int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void product_thin(const ProductArgs a) {
+    typedef typename Vec<T>::v8 v8;
+    typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+    __shared__ float sums[WAVES][256];
+    const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6);
+    const uint32_t p0 = blockIdx.x * 16, line = lane & 15;
+    constexpr int SIZE = EIGHT ? 1 : 2;
+    constexpr uint32_t NOWHERE = 0x80000000u;
+    const __amdgpu_buffer_rsrc_t rp = __builtin_amdgcn_make_buffer_rsrc((char*)a.p.d + p0 * a.p.ld * SIZE, 0, NOWHERE - 1, 0x00020000);
+    const __amdgpu_buffer_rsrc_t rq = __builtin_amdgcn_make_buffer_rsrc((void*)a.q.d, 0, NOWHERE - 1, 0x00020000);
+    const uint32_t at = (lane >> 4) * 16;
+    const uint32_t op = p0 + line < a.np ? (uint32_t)(line * a.p.ld + at) * SIZE : NOWHERE, oq = line < a.nq ? (uint32_t)(line * a.q.ld + at) * 2 : NOWHERE;
+    f4 acc = {0, 0, 0, 0};
+    constexpr int AHEAD = EIGHT ? 8 : 4;
+    const uint32_t chunks = (a.nr + 63) / 64;
+    for (uint32_t c = w; c < chunks; c += WAVES * AHEAD) {
+        u4 x[AHEAD][EIGHT ? 1 : 2], y[AHEAD][2];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const uint32_t r = (c + i * WAVES) * 64;
+            const bool in = r + at < a.nr;
+            const uint32_t fp = in ? op : NOWHERE, fq = in ? oq : NOWHERE;
+            const uint32_t sp = in || c + i * WAVES < chunks ? r * SIZE : 0, sq = c + i * WAVES < chunks ? r * 2 : 0;
+            x[i][0] = __builtin_amdgcn_raw_buffer_load_b128(rp, fp, sp, 0);
+            if (!EIGHT) x[i][EIGHT ? 0 : 1] = __builtin_amdgcn_raw_buffer_load_b128(rp, fp == NOWHERE ? NOWHERE : fp + 16, sp, 0);
+            y[i][0] = __builtin_amdgcn_raw_buffer_load_b128(rq, fq, sq, 0);
+            y[i][1] = __builtin_amdgcn_raw_buffer_load_b128(rq, fq == NOWHERE ? NOWHERE : fq + 16, sq, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            v8 lo, hi;
+            if (EIGHT) {
+                lo = widen<T>(x[i][0][0], x[i][0][1]);
+                hi = widen<T>(x[i][0][2], x[i][0][3]);
+            } else {
+                lo = __builtin_bit_cast(v8, x[i][0]);
+                hi = __builtin_bit_cast(v8, x[i][EIGHT ? 0 : 1]);
+            }
+            acc = mfma<T>(lo, __builtin_bit_cast(v8, y[i][0]), acc);
+            acc = mfma<T>(hi, __builtin_bit_cast(v8, y[i][1]), acc);
+        }
+    }
+    /* acc: q = lane & 15, p from 4 (lane >> 4) on */
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sums[w][(lane & 15) * 16 + (lane >> 4) * 4 + i] = acc[i];
+    __syncthreads();
+    if (t >= 32) return;
+    const uint32_t q = t >> 1, p = (t & 1) * 8;
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        v[i] = sums[0][q * 16 + p + i];
+        for (int k = 1; k < WAVES; ++k) v[i] += sums[k][q * 16 + p + i];
+    }
+    finish8<T, true>(a, q, p0 + p, v);
 }
 
 /* ---- the gradient before the activation ------------------------------------------------------------------

@@ -123,7 +123,7 @@ inline void norm_backward(int dtype, int kind, const tc_matrix* dy, const tc_mat
         if (dbeta) dbeta[c] = (float)db[c];
     }
 }
-inline void linear(int dtype, const tc_matrix* x, const tc_matrix* w, const void* bias, int act, const tc_matrix* residual, const tc_matrix* y, const tc_matrix* z) {
+inline void linear(int dtype, const tc_matrix* x, const tc_matrix* w, const void* bias, int act, const tc_matrix* residual, const tc_matrix* y, const tc_matrix* z, void*) {
     for (size_t r = 0; r < x->rows; ++r)
         for (size_t o = 0; o < w->rows; ++o) {
             double v = bias ? load16(bias, o, dtype) : 0;

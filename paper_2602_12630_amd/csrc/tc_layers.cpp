@@ -74,12 +74,58 @@ uint32_t slope_groups(uint32_t rows, uint32_t cols) {
     const uint32_t strips = (cols + 511) / 512;
     return std::max<uint32_t>(1, std::min<uint32_t>((2048 + strips - 1) / strips, (rows + 15) / 16));
 }
+/* How a product of np x nq results over nr is laid out: the tile, and into how many parts r is split so that there are workgroups for
+ * the whole chip. */
+struct ProductPlan {
+    uint32_t np, nq, side_p, side_q, splits, r_split;
+    uint64_t ldp;
+    uint64_t tiles(uint32_t sp, uint32_t sq) const { return (uint64_t)((np + sp - 1) / sp) * ((nq + sq - 1) / sq); }
+    size_t part_bytes() const { return splits > 1 ? (size_t)splits * nq * ldp * 4 : 0; }
+    /* with the 16-bit copy of an int8 operand, which the kernel of the largest tiles wants */
+    size_t bytes(uint32_t nr) const { return part_bytes() + (side_p == 256 ? up((size_t)np * nr * 2, 256) : 0); }
+};
+/* Chosen by what the layouts cost, in microseconds, measured over products of 10^9 to 10^12 multiply-adds: so much for a step of 64 r
+ * with one, two .. workgroups on every compute unit (as many as LDS holds), one for a round of workgroups to start and finish in, and
+ * for a split the writing and reading of its parts at 6 GB a millisecond and one more launch.  Within 10 % of the best layout
+ * wherever both were timed: 8192 x 4096 -> 11008: 256 x 256 641 us, 128 x 128 672, 64 x 64 992; 487 x 11008 -> 4096: 128 x 128 in four parts
+ * 52 us, whole 114, 256 x 256 in eight parts 61; 64 x 4096 -> 4096: 64 x 64 in eight parts 15 us, whole 33, 128 x 128 whole 42. */
+ProductPlan product_plan(uint32_t np, uint32_t nq, uint32_t nr) {
+    struct Layout {
+        uint32_t side, deepest;
+        double step[5];
+    };
+    static const Layout layouts[3] = {{256, 1, {1.8}}, {128, 2, {0.75, 0.97}}, {64, 5, {0.48, 0.5, 0.62, 0.75, 0.9}}};
+    static const uint32_t parts[] = {1, 2, 3, 4, 6, 8, 12, 16};
+    ProductPlan best = {np, nq, 64, 64, 1, nr, up(np, 8)};
+    double least = 1e300;
+    for (const Layout& l : layouts)
+        for (uint32_t splits : parts) {
+            ProductPlan p = {np, nq, l.side, l.side, 1, nr, up(np, 8)};
+            if (splits > 1) {
+                p.r_split = (uint32_t)up((nr + splits - 1) / splits, 64);
+                p.splits = (nr + p.r_split - 1) / p.r_split;
+                if (p.splits != splits || p.r_split < 256) break;
+            }
+            const double groups = (double)p.tiles(l.side, l.side) * splits, steps = (p.r_split + 63) / 64;
+            const uint32_t deep = (uint32_t)std::min<double>(l.deepest, std::ceil(groups / 256));
+            double rounds = groups / (256.0 * deep);
+            if (rounds < 3) rounds = std::ceil(rounds);
+            double cost = rounds * (steps * l.step[deep - 1] + 1);
+            if (splits > 1) cost += 4 + (double)p.part_bytes() * 2 / 6e6;
+            if (cost < least) {
+                least = cost;
+                best = p;
+            }
+        }
+    return best;
+}
 /* workspace of the linear gradients: where each part lies */
 struct BackPlan {
-    size_t by_x, by_w, part, m, bytes;
+    size_t by_x, by_w, part, m, split, bytes;
     uint64_t ld_by;
 };
-BackPlan back_plan(uint32_t rows, uint32_t out) {
+/* in = 0: neither dx nor dw is wanted */
+BackPlan back_plan(uint32_t rows, uint32_t in, uint32_t out) {
     BackPlan b;
     b.ld_by = up(out, 8);
     const size_t scaled = up((size_t)rows * b.ld_by * 2, 256);
@@ -87,7 +133,8 @@ BackPlan back_plan(uint32_t rows, uint32_t out) {
     b.by_w = scaled;
     b.part = 2 * scaled;
     b.m = b.part + up((size_t)slope_groups(rows, out) * out * 4, 256);
-    b.bytes = b.m + 256;
+    b.split = b.m + 256;
+    b.bytes = b.split + (in ? std::max(product_plan(in, rows, out).bytes(out), product_plan(in, out, rows).bytes(rows)) : 0);
     return b;
 }
 
@@ -98,7 +145,7 @@ namespace {
 using namespace tc::layers;
 #define LAUNCH(kernel, grid, block, lds, args)                                              \
     do {                                                                                    \
-        hipLaunchKernelGGL(kernel, grid, dim3(block), lds, ctx_stream(ctx), args);          \
+        hipLaunchKernelGGL(kernel, dim3(grid), dim3(block), lds, ctx_stream(ctx), args);          \
         int e_ = (int)hipGetLastError();                                                    \
         if (e_) return ctx_fail_hip(ctx, e_, "launch of " #kernel);                         \
     } while (0)
@@ -110,26 +157,28 @@ bool wide(const void* p, uint64_t ld, uint32_t rows, uint32_t cols, int dtype) {
 }
 bool wide(const tc_matrix* m) { return wide(m->d_data, m->ld, m->rows, m->cols, m->dtype); }
 
+/* workgroups for `sets` sets of rows; the kernels go round until all are done */
+uint32_t row_grid(uint64_t sets) { return (uint32_t)std::min<uint64_t>(sets, 1u << 20); }
 template <class T, bool WIDE>
 int encode_rows(tc_ctx* ctx, const RowArgs& a) {
     const uint32_t c = a.cols;
-    if (c <= 512) LAUNCH((checkpoint_encode<T, WIDE, 64, 1>), dim3((a.rows + 3) / 4), 256, 0, a);
-    else if (c <= 2048) LAUNCH((checkpoint_encode<T, WIDE, 256, 1>), dim3(a.rows), 256, 0, a);
-    else if (c <= 4096) LAUNCH((checkpoint_encode<T, WIDE, 256, 2>), dim3(a.rows), 256, 0, a);
-    else if (c <= 8192) LAUNCH((checkpoint_encode<T, WIDE, 256, 4>), dim3(a.rows), 256, 0, a);
-    else if (c <= 16384) LAUNCH((checkpoint_encode<T, WIDE, 256, 8>), dim3(a.rows), 256, 0, a);
-    else LAUNCH((checkpoint_encode<T, WIDE, 1024, 0>), dim3(a.rows), 1024, 0, a);
+    if (c <= 512) LAUNCH((checkpoint_encode<T, WIDE, 64, 1>), row_grid(((uint64_t)a.rows + 3) / 4), 256, 0, a);
+    else if (c <= 2048) LAUNCH((checkpoint_encode<T, WIDE, 256, 1>), row_grid(a.rows), 256, 0, a);
+    else if (c <= 4096) LAUNCH((checkpoint_encode<T, WIDE, 256, 2>), row_grid(a.rows), 256, 0, a);
+    else if (c <= 8192) LAUNCH((checkpoint_encode<T, WIDE, 256, 4>), row_grid(a.rows), 256, 0, a);
+    else if (c <= 16384) LAUNCH((checkpoint_encode<T, WIDE, 256, 8>), row_grid(a.rows), 256, 0, a);
+    else LAUNCH((checkpoint_encode<T, WIDE, 1024, 0>), row_grid(a.rows), 1024, 0, a);
     return TC_OK;
 }
 template <class T, bool WIDE>
 int norm_rows(tc_ctx* ctx, const NormArgs& a) {
     const uint32_t c = a.cols;
-    if (c <= 512) LAUNCH((norm_forward<T, WIDE, 64, 1>), dim3((a.rows + 3) / 4), 256, 0, a);
-    else if (c <= 2048) LAUNCH((norm_forward<T, WIDE, 256, 1>), dim3(a.rows), 256, 0, a);
-    else if (c <= 4096) LAUNCH((norm_forward<T, WIDE, 256, 2>), dim3(a.rows), 256, 0, a);
-    else if (c <= 8192) LAUNCH((norm_forward<T, WIDE, 256, 4>), dim3(a.rows), 256, 0, a);
-    else if (c <= 16384) LAUNCH((norm_forward<T, WIDE, 1024, 2>), dim3(a.rows), 1024, 0, a);
-    else LAUNCH((norm_forward<T, WIDE, 1024, 4>), dim3(a.rows), 1024, 0, a);
+    if (c <= 512) LAUNCH((norm_forward<T, WIDE, 64, 1>), row_grid(((uint64_t)a.rows + 3) / 4), 256, 0, a);
+    else if (c <= 2048) LAUNCH((norm_forward<T, WIDE, 256, 1>), row_grid(a.rows), 256, 0, a);
+    else if (c <= 4096) LAUNCH((norm_forward<T, WIDE, 256, 2>), row_grid(a.rows), 256, 0, a);
+    else if (c <= 8192) LAUNCH((norm_forward<T, WIDE, 256, 4>), row_grid(a.rows), 256, 0, a);
+    else if (c <= 16384) LAUNCH((norm_forward<T, WIDE, 1024, 2>), row_grid(a.rows), 1024, 0, a);
+    else LAUNCH((norm_forward<T, WIDE, 1024, 4>), row_grid(a.rows), 1024, 0, a);
     return TC_OK;
 }
 template <class T, bool WIDE>
@@ -157,11 +206,60 @@ int clear_rows(tc_ctx* ctx, void* out, uint64_t ld, uint32_t rows, uint32_t cols
     int e = (int)hipGetLastError();
     return e ? ctx_fail_hip(ctx, e, "launch of fill_rows") : TC_OK;
 }
-template <class T, bool P_ALONG, bool P_EIGHT, bool Q_ALONG, bool Q_EIGHT, bool FORWARD>
-int multiply(tc_ctx* ctx, const ProductArgs& a) {
-    const uint64_t tiles = (uint64_t)((a.np + 127) / 128) * ((a.nq + 127) / 128);
-    if (tiles > 0x7FFFFFFFu) REFUSE(TC_ERR_SHAPE, "product too large");
-    LAUNCH((product<T, P_ALONG, P_EIGHT, Q_ALONG, Q_EIGHT, FORWARD>), dim3((uint32_t)tiles), 256, 0, a);
+/* whether an operand can be read in pieces of eight elements (sixteen: `twice`): aligned rows of whole pieces, and a tile's addresses within 31 bits */
+bool in_pieces(const Operand& o, uint32_t along_memory, bool eight, bool twice = false) {
+    const uint32_t piece = twice ? 16 : 8;
+    return ((uintptr_t)o.d & (eight ? piece - 1 : 15u)) == 0 && o.ld % piece == 0 && along_memory % piece == 0 && o.ld < (1u << 21);
+}
+template <class K>
+int launch_product(tc_ctx* ctx, K* kernel, const ProductArgs& a, uint64_t grid, int threads, size_t lds) {
+    if (grid * threads > 0xFFFFFFFFull) REFUSE(TC_ERR_SHAPE, "product too large for one launch");
+    LAUNCH(kernel, (uint32_t)grid, threads, lds, a);
+    return TC_OK;
+}
+/* kernels that use more than the 64 KB of LDS that every kernel may */
+#define LARGE_LDS(kernel, bytes)                                                                                                     \
+    do {                                                                                                                             \
+        static const int e_ = (int)hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)(bytes)); \
+        if (e_) return ctx_fail_hip(ctx, e_, "LDS of a product");                                                                    \
+    } while (0)
+template <class T, bool P_ALONG, bool P_EIGHT, bool Q_ALONG, bool FORWARD>
+int multiply(tc_ctx* ctx, ProductArgs a, float* part) {
+    const bool pieces = in_pieces(a.p, P_ALONG ? a.nr : a.np, P_EIGHT) && in_pieces(a.q, Q_ALONG ? a.nr : a.nq, false);
+    if (FORWARD && a.nq <= 16 && pieces && in_pieces(a.p, a.nr, P_EIGHT, true) && in_pieces(a.q, a.nr, false, true))
+        return launch_product(ctx, product_thin<T, P_EIGHT, 8>, a, (a.np + 15) / 16, 512, 0);
+    const ProductPlan plan = product_plan(a.np, a.nq, a.nr);
+    if (!pieces) return launch_product(ctx, product<T, P_ALONG, P_EIGHT, Q_ALONG, FORWARD>, a, plan.tiles(128, 128), 256, 0);
+    a.r_split = plan.r_split;
+    if (plan.splits > 1) {
+        a.part = part;
+        a.ldp = plan.ldp;
+    }
+    const uint64_t grid = plan.tiles(plan.side_p, plan.side_q) * plan.splits;
+    if (plan.side_p == 256) {
+        if (P_EIGHT) {
+            const uint32_t lines = P_ALONG ? a.np : a.nr, cols = P_ALONG ? a.nr : a.np;
+            T* wide = (T*)((uint8_t*)part + plan.part_bytes());
+            hipLaunchKernelGGL(widen_rows<T>, dim3((cols + 2047) / 2048, std::min<uint32_t>(lines, 65535)), dim3(256), 0, ctx_stream(ctx), a.p, wide, cols, lines, cols);
+            int e = (int)hipGetLastError();
+            if (e) return ctx_fail_hip(ctx, e, "launch of widen_rows");
+            a.p = Operand{wide, cols};
+        }
+        const size_t lds = 5 * 512 * 32 * 2;
+        auto* kernel = product_deep<T, P_ALONG, Q_ALONG, FORWARD, 256, 256, 2, 4>;
+        LARGE_LDS(kernel, lds);
+        TRY(launch_product(ctx, kernel, a, grid, 512, lds));
+    } else if (plan.side_p == 128) {
+        TRY(launch_product(ctx, product_paired<T, P_ALONG, P_EIGHT, Q_ALONG, FORWARD, 128, 128, 2, 2>, a, grid, 256, 2 * 256 * 64 * 2));
+    } else {
+        TRY(launch_product(ctx, product_paired<T, P_ALONG, P_EIGHT, Q_ALONG, FORWARD, 64, 64, 2, 2>, a, grid, 256, 2 * 128 * 64 * 2));
+    }
+    if (plan.splits > 1) {
+        const uint64_t pieces8 = (uint64_t)((a.np + 7) / 8) * a.nq;
+        hipLaunchKernelGGL((join_parts<T, FORWARD>), dim3((uint32_t)((pieces8 + 255) / 256)), dim3(256), 0, ctx_stream(ctx), a, plan.splits);
+        int e = (int)hipGetLastError();
+        if (e) return ctx_fail_hip(ctx, e, "launch of join_parts");
+    }
     return TC_OK;
 }
 
@@ -173,10 +271,9 @@ int run_encode(tc_ctx* ctx, const tc_matrix* src, const tc_matrix* dst) {
 template <class T>
 int run_decode(tc_ctx* ctx, const tc_matrix* src, const tc_matrix* dst) {
     const RowArgs a{src->d_data, dst->d_data, src->d_scale, src->ld, dst->ld, src->rows, src->cols};
-    const uint64_t grid = (uint64_t)a.rows * ((a.cols + 2047) / 2048);
-    if (grid > 0x7FFFFFFFu) REFUSE(TC_ERR_SHAPE, "matrix too large");
-    if (wide(src) && wide(dst)) LAUNCH((checkpoint_decode<T, true>), dim3((uint32_t)grid), 256, 0, a);
-    else LAUNCH((checkpoint_decode<T, false>), dim3((uint32_t)grid), 256, 0, a);
+    const dim3 grid((a.cols + 2047) / 2048, std::min<uint32_t>(a.rows, 65535));
+    if (wide(src) && wide(dst)) LAUNCH((checkpoint_decode<T, true>), grid, 256, 0, a);
+    else LAUNCH((checkpoint_decode<T, false>), grid, 256, 0, a);
     return TC_OK;
 }
 template <class T>
@@ -199,7 +296,8 @@ int run_norm_backward(tc_ctx* ctx, int kind, const tc_matrix* dy, const tc_matri
     return TC_OK;
 }
 template <class T>
-int run_linear(tc_ctx* ctx, const tc_matrix* x, const tc_matrix* w, const void* bias, int act, const tc_matrix* residual, const tc_matrix* y, const tc_matrix* z) {
+int run_linear(tc_ctx* ctx, const tc_matrix* x, const tc_matrix* w, const void* bias, int act, const tc_matrix* residual, const tc_matrix* y, const tc_matrix* z,
+               void* ws) {
     ProductArgs a = {};
     a.p = Operand{w->d_data, w->ld};
     a.q = Operand{x->d_data, x->ld};
@@ -213,15 +311,16 @@ int run_linear(tc_ctx* ctx, const tc_matrix* x, const tc_matrix* w, const void* 
     if (residual) { a.residual = residual->d_data; a.ldres = residual->ld; }
     if (z) { a.z = z->d_data; a.ldz = z->ld; }
     a.act = act;
-    return a.p_scale ? multiply<T, true, true, true, false, true>(ctx, a) : multiply<T, true, false, true, false, true>(ctx, a);
+    a.wide_out = wide(y) && (!residual || wide(residual)) && (!z || wide(z)) && ((uintptr_t)bias & 15u) == 0;
+    return a.p_scale ? multiply<T, true, true, true, true>(ctx, a, (float*)ws) : multiply<T, true, false, true, true>(ctx, a, (float*)ws);
 }
 template <class T>
 int run_linear_backward(tc_ctx* ctx, const tc_matrix* dy, const tc_matrix* x, const tc_matrix* w, int act, const tc_matrix* z, const tc_matrix* dz,
                         const tc_matrix* dx, const tc_matrix* dw, float* dbias, void* ws) {
     const uint32_t rows = dy->rows, out = dy->cols;
-    const BackPlan plan = back_plan(rows, out);
+    const BackPlan plan = back_plan(rows, dx ? dx->cols : dw ? dw->cols : 0, out);
     uint8_t* base = (uint8_t*)ws;
-    float* m = (float*)(base + plan.m);
+    float *m = (float*)(base + plan.m), *parts = (float*)(base + plan.split);
     const bool by_x = dw && x->dtype == TC_I8, by_w = dx && w->dtype == TC_I8;
     if (by_x || by_w) {
         hipLaunchKernelGGL(scale_peak, dim3(2), dim3(1024), 0, ctx_stream(ctx), by_x ? x->d_scale : nullptr, rows, by_w ? w->d_scale : nullptr, out, m);
@@ -267,8 +366,9 @@ int run_linear_backward(tc_ctx* ctx, const tc_matrix* dy, const tc_matrix* x, co
         a.nr = out;
         a.out = dx->d_data;
         a.ldo = dx->ld;
+        a.wide_out = wide(dx);
         a.factor = by_w ? m + 2 : nullptr;
-        TRY((by_w ? multiply<T, false, true, true, false, false>(ctx, a) : multiply<T, false, false, true, false, false>(ctx, a)));
+        TRY((by_w ? multiply<T, false, true, true, false>(ctx, a, parts) : multiply<T, false, false, true, false>(ctx, a, parts)));
     }
     if (dw) {
         ProductArgs a = {};
@@ -279,8 +379,9 @@ int run_linear_backward(tc_ctx* ctx, const tc_matrix* dy, const tc_matrix* x, co
         a.nr = rows;
         a.out = dw->d_data;
         a.ldo = dw->ld;
+        a.wide_out = wide(dw);
         a.factor = by_x ? m : nullptr;
-        TRY((by_x ? multiply<T, false, true, false, false, false>(ctx, a) : multiply<T, false, false, false, false, false>(ctx, a)));
+        TRY((by_x ? multiply<T, false, true, false, false>(ctx, a, parts) : multiply<T, false, false, false, false>(ctx, a, parts)));
     }
     return TC_OK;
 }
@@ -382,7 +483,7 @@ static bool linear_sizes(uint32_t rows, uint32_t in, uint32_t out) {
 extern "C" int tc_linear_workspace(uint32_t rows, uint32_t in, uint32_t out, size_t* bytes) {
     if (!bytes) return TC_ERR_ARG;
     if (!linear_sizes(rows, in, out)) return TC_ERR_SHAPE;
-    *bytes = 0;
+    *bytes = product_plan(out, rows, in).bytes(in);
     return TC_OK;
 }
 extern "C" int tc_linear(tc_ctx* ctx, const tc_matrix* x, const tc_matrix* w, const void* d_bias, int activation, const tc_matrix* residual,
@@ -407,12 +508,12 @@ extern "C" int tc_linear(tc_ctx* ctx, const tc_matrix* x, const tc_matrix* w, co
     TRY(check_workspace(ctx, d_workspace, workspace_bytes, need));
     if (!x->rows) return TC_OK;
     TRY(ctx_use_device(ctx));
-    return RUN(linear, x->dtype, x, w, d_bias, activation, residual, y, z);
+    return RUN(linear, x->dtype, x, w, d_bias, activation, residual, y, z, d_workspace);
 }
 extern "C" int tc_linear_backward_workspace(uint32_t rows, uint32_t in, uint32_t out, size_t* bytes) {
     if (!bytes) return TC_ERR_ARG;
     if (!linear_sizes(rows, in, out)) return TC_ERR_SHAPE;
-    *bytes = back_plan(rows, out).bytes;
+    *bytes = back_plan(rows, in, out).bytes;
     return TC_OK;
 }
 extern "C" int tc_linear_backward(tc_ctx* ctx, const tc_matrix* dy, const tc_matrix* x, const tc_matrix* w, int activation, const tc_matrix* z,
@@ -422,7 +523,7 @@ extern "C" int tc_linear_backward(tc_ctx* ctx, const tc_matrix* dy, const tc_mat
     if (activation < TC_ACT_NONE || activation > TC_ACT_SILU) REFUSE(TC_ERR_ARG, "unknown activation");
     TRY(check_view(ctx, dy, false));
     const uint32_t rows = dy->rows, out = dy->cols;
-    uint32_t in = 1;
+    uint32_t in = 0;
     if (activation == TC_ACT_NONE) {
         if (z || dz) REFUSE(TC_ERR_ARG, "without an activation z and dz must be null");
     } else {
@@ -453,9 +554,7 @@ extern "C" int tc_linear_backward(tc_ctx* ctx, const tc_matrix* dy, const tc_mat
         TRY(check_shape(ctx, x, rows, in));
     }
     TRY(check_vector(ctx, d_dbias, 4));
-    size_t need = 0;
-    TRY(tc_linear_backward_workspace(rows, in, out, &need));
-    TRY(check_workspace(ctx, d_workspace, workspace_bytes, need));
+    TRY(check_workspace(ctx, d_workspace, workspace_bytes, back_plan(rows, in, out).bytes));
     TRY(ctx_use_device(ctx));
     if (!rows) {
 #if !defined(TC_HOST_EMU)

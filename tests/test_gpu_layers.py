@@ -603,3 +603,70 @@ def test_offsets_past_32_bits(T, ctx):
     ok(dx, d @ w64, e["dx"])
     ok(dw, d.t() @ x64, e["dw"])
     assert torch.equal(q, ref.encode(x)[0])
+
+
+# every layout of a product and every way of splitting it: sizes at which each of them is the cheapest for one of the three products
+LARGE = [(8200, 136, 8456), (8200, 8456, 136), (136, 8456, 8200), (487, 4104, 4104), (4104, 1040, 1040), (300, 4104, 520), (200, 200, 4104), (1100, 2056, 520)]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("rows,k,n", LARGE)
+def test_products_of_every_layout(T, ctx, dtype, eight, rows, k, n):
+    t = ref.DT[dtype]
+    seed = rows + 5 * k + 7 * n
+    x, mw, w64 = linear_inputs(T, t, rows, k, n, eight, seed, (0, 0))
+    work = space(ctx.linear_workspace(rows, k, n))
+    work.fill_(0xFF)
+    bias = rand((n,), seed + 2, t)
+    ybuf, y = empty(rows, n, t)
+    z = torch.empty(rows, n, dtype=t, device="cuda")
+    ctx.linear(T.Matrix(x), mw, T.Matrix(y), bias=bias, activation=T.TC_ACT_GELU, z=T.Matrix(z), workspace=work)
+    ctx.sync()
+    z64 = x.double() @ w64.t() + bias.double()
+    ez = ref.product_error(x.double().abs() @ w64.abs().t() + bias.double().abs(), k + 2)
+    ok(z, z64, ez + ref.u(t) * (z64.abs() + ez) + ref.tiny(t))
+    y64 = ref.activate(z64, "gelu")
+    ey = 1.13 * ez + ref.activation_error(z64, "gelu")
+    ok(y, y64, ey + ref.u(t) * (y64.abs() + ey) + ref.tiny(t))
+    assert untouched(ybuf, rows, n)
+    del z64, ez, y64, ey
+    mx, x64, qx, m_x = T.Matrix(x), ref.value(x), None, None
+    if eight:
+        q, s = rows8(x)
+        mx, x64, qx, m_x = T.Matrix(q, s), ref.value(q, s), q.double(), power_above(s)
+    m_w, qw = (power_above(mw.scale), mw.tensor.double()) if eight else (None, None)
+    dy = rand((rows, n), seed + 5, t)
+    dxbuf, dx = empty(rows, k, t)
+    dwbuf, dw = empty(n, k, t)
+    db = torch.empty(n, device="cuda")
+    work = space(ctx.linear_backward_workspace(rows, k, n))
+    work.fill_(0xFF)
+    ctx.linear_backward(T.Matrix(dy), mx, mw, dx=T.Matrix(dx), dw=T.Matrix(dw), dbias=db, workspace=work)
+    ctx.sync()
+    d64 = dy.double()
+    dx64, dw64 = d64 @ w64, d64.t() @ x64
+    e = backward_bounds(d64, torch.zeros_like(d64), "none", t, w64, x64, m_w, m_x, qw, qx, dx64, dw64)
+    ok(dx, dx64, e["dx"])
+    ok(dw, dw64, e["dw"])
+    ok(db, d64.sum(0), e["dbias"])
+    assert untouched(dxbuf, rows, k) and untouched(dwbuf, n, k)
+
+
+def test_more_rows_than_a_launch_has_workgroups(T, ctx):
+    t = torch.float16
+    rows = (1 << 24) + 77
+    x = rand((rows, 8), 1, t)
+    q, s, back, y = torch.empty(rows, 8, dtype=torch.int8, device="cuda"), torch.empty(rows, device="cuda"), torch.empty_like(x), torch.empty_like(x)
+    ctx.checkpoint_encode(T.Matrix(x), T.Matrix(q, s))
+    ctx.checkpoint_decode(T.Matrix(q, s), T.Matrix(back))
+    ctx.norm(1, T.Matrix(x), None, None, 1e-5, T.Matrix(y))
+    ctx.sync()
+    want, scale = ref.encode(x)
+    assert torch.equal(q, want) and torch.equal(s, scale)
+    v = ref.value(want, scale)
+    ok(back, v, (ref.u(t) + 2 * ref.E) * v.abs() + ref.tiny(t))
+    del v
+    x64 = x.double()
+    want, _, rstd = ref.norm(x64, None, None, 1e-5, False)
+    ok(y, want, ref.norm_bound(x64, None, None, want, rstd, t, False))
