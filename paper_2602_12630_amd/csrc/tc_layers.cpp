@@ -97,6 +97,7 @@ ProductPlan product_plan(uint32_t np, uint32_t nq, uint32_t nr) {
     static const Layout layouts[3] = {{256, 1, {1.8}}, {128, 2, {0.75, 0.97}}, {64, 5, {0.48, 0.5, 0.62, 0.75, 0.9}}};
     static const uint32_t parts[] = {1, 2, 3, 4, 6, 8, 12, 16};
     ProductPlan best = {np, nq, 64, 64, 1, nr, up(np, 8)};
+    if (!nq || !nr) return best;                     /* no rows: nothing is launched */
     double least = 1e300;
     for (const Layout& l : layouts)
         for (uint32_t splits : parts) {
