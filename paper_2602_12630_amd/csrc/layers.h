@@ -6,6 +6,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 namespace tc {
 namespace layers {
 
@@ -19,55 +21,70 @@ typedef int8_t q8 __attribute__((ext_vector_type(8)));
 /* ---- activations: value and slope ------------------------------------------------------------------
  * Phi(z) by the rational form 7.1.26 of Abramowitz and Stegun's handbook: the upper tail of the normal distribution is
  * t (a1 + t (a2 + ..)) exp(-z^2 / 2) / 2 with t = 1 / (1 + p |z| / sqrt 2), within 7.5e-8 of it everywhere, which is the
- * size of a float32 rounding of Phi: 12 operations where the library's erf takes some 40.  Products with a factor that has
- * become 0 are 0, also at z = +-infinity, so that an overflowed value before the activation does not turn into a NaN. */
-__device__ __forceinline__ float normal_tail(float z, float& bell) {
-    const float a = fabsf(z) * 0.70710678118654752f;
-    const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, a, 1.0f));
-    bell = __expf(-0.5f * z * z);
-    const float p = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
-    return 0.5f * p * bell;
+ * size of a float32 rounding of Phi.  gelu = max(z, 0) - |z| tail: some 22 operations, where the library's erf alone takes 40; in the epilogue
+ * of a product of 8192 x 4096 -> 11008 they cost what is left in DESIGN_GELU.  |z| is held at 14, beyond which every factor has
+ * become 0, so that infinities (values before the activation that overflowed) do not turn into NaNs; NaNs stay. */
+__device__ __forceinline__ float held_at_14(float z) {
+    const float a = fabsf(z);
+    return a > 14.0f ? 14.0f : a;
 }
-__device__ __forceinline__ float times(float z, float f) { return f == 0.0f ? 0.0f : z * f; }
+__device__ __forceinline__ float normal_tail(float a, float& bell) {
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678118654752f, a, 1.0f));
+    bell = __builtin_amdgcn_exp2f(-0.72134752044448170f * (a * a));
+    return bell * (t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f), 0.5f * 1.421413741f), 0.5f * -0.284496736f), 0.5f * 0.254829592f));
+}
+__device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.4426950408889634f * z)); }
 __device__ __forceinline__ float activate(float z, int act) {
-    if (act == TC_ACT_RELU) return z > 0.0f ? z : (z != z ? z : 0.0f);
+    if (act == TC_ACT_RELU) return z < 0.0f ? 0.0f : z;
     if (act == TC_ACT_GELU) {
         float bell;
-        const float tail = normal_tail(z, bell);
-        return times(z, z > 0.0f ? 1.0f - tail : tail);
+        const float a = held_at_14(z);
+        return fmaf(-a, normal_tail(a, bell), z < 0.0f ? 0.0f : z);
     }
-    if (act == TC_ACT_SILU) return times(z, __builtin_amdgcn_rcpf(1.0f + __expf(-z)));
+    if (act == TC_ACT_SILU) return (z < -104.0f ? -104.0f : z) * sigmoid(z);
     return z;
 }
 __device__ __forceinline__ float slope(float z, int act) {
     if (act == TC_ACT_RELU) return z > 0.0f ? 1.0f : (z != z ? z : 0.0f);
     if (act == TC_ACT_GELU) {
         float bell;
-        const float tail = normal_tail(z, bell);
-        return (z > 0.0f ? 1.0f - tail : tail) + times(z, 0.3989422804014327f * bell);
+        const float a = held_at_14(z), tail = normal_tail(a, bell);
+        return fmaf(copysignf(a, z), 0.3989422804014327f * bell, z < 0.0f ? tail : 1.0f - tail);
     }
     if (act == TC_ACT_SILU) {
-        const float s = __builtin_amdgcn_rcpf(1.0f + __expf(-z));
-        return s + times(z, s * (1.0f - s));
+        const float s = sigmoid(z), far = z < -104.0f ? -104.0f : z > 104.0f ? 104.0f : z;
+        return fmaf(far, s * (1.0f - s), s);
     }
     return 1.0f;
 }
 
-/* ---- sums and maxima of a wave or of the waves that share a row -------------------------------------- */
+/* ---- sums and maxima of a wave or of the waves that share a row --------------------------------------
+ * Within sixteen lanes by moves between neighbours (one instruction each, no LDS), the four sixteens through scalar registers. */
+template <int CTRL>
+__device__ __forceinline__ float moved(float v) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));
+}
+__device__ __forceinline__ float lane_of(float v, int l) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), l)); }
 __device__ __forceinline__ float wave_sum(float v) {
-    for (int k = 32; k; k >>= 1) v += __shfl_xor(v, k, 64);
-    return v;
+    v += moved<0xB1>(v);         /* the other one of a pair, the other pair of four */
+    v += moved<0x4E>(v);
+    v += moved<0x141>(v);        /* eight lanes mirrored, sixteen lanes mirrored */
+    v += moved<0x140>(v);
+    return (lane_of(v, 0) + lane_of(v, 16)) + (lane_of(v, 32) + lane_of(v, 48));
 }
 __device__ __forceinline__ float wave_max(float v) {
-    for (int k = 32; k; k >>= 1) v = fmaxf(v, __shfl_xor(v, k, 64));
-    return v;
+    v = fmaxf(v, moved<0xB1>(v));
+    v = fmaxf(v, moved<0x4E>(v));
+    v = fmaxf(v, moved<0x141>(v));
+    v = fmaxf(v, moved<0x140>(v));
+    return fmaxf(fmaxf(lane_of(v, 0), lane_of(v, 16)), fmaxf(lane_of(v, 32), lane_of(v, 48)));
 }
-/* TH lanes of the workgroup (TH / 64 whole waves) together; cells: TH / 64 floats of LDS of this group.  Every lane of the workgroup calls it. */
+/* TH lanes of the workgroup (TH / 64 whole waves) together.  cells: TH / 64 floats of LDS of this group that nobody else uses between this
+ * call's barrier and a later one; every lane of the workgroup makes the call. */
 template <int TH>
 __device__ __forceinline__ float group_sum(float v, float* cells, int t) {
     v = wave_sum(v);
     if (TH == 64) return v;
-    __syncthreads();
     if ((t & 63) == 0) cells[t >> 6] = v;
     __syncthreads();
     v = cells[0];
@@ -78,12 +95,26 @@ template <int TH>
 __device__ __forceinline__ float group_max(float v, float* cells, int t) {
     v = wave_max(v);
     if (TH == 64) return v;
-    __syncthreads();
     if ((t & 63) == 0) cells[t >> 6] = v;
     __syncthreads();
     v = cells[0];
     for (int w = 1; w < TH / 64; ++w) v = fmaxf(v, cells[w]);
     return v;
+}
+/* two sums at one barrier */
+template <int TH>
+__device__ __forceinline__ void group_sum2(float& u, float& v, float2* cells, int t) {
+    u = wave_sum(u);
+    v = wave_sum(v);
+    if (TH == 64) return;
+    if ((t & 63) == 0) cells[t >> 6] = make_float2(u, v);
+    __syncthreads();
+    u = cells[0].x;
+    v = cells[0].y;
+    for (int w = 1; w < TH / 64; ++w) {
+        u += cells[w].x;
+        v += cells[w].y;
+    }
 }
 
 /* ---- rows in registers -------------------------------------------------------------------------------
@@ -137,6 +168,59 @@ __device__ __forceinline__ void store8(T* p, int t, int c, uint32_t cols, const 
     }
 }
 
+/* the same in two steps, so that several loads can be under way: raw bits, then values */
+template <class T, int TH, bool WIDE>
+struct Raw {
+    uint32_t w[4];
+    __device__ __forceinline__ void load(const T* p, int t, int c, uint32_t cols) {
+        if (WIDE) {
+            const uint32_t k = row_col<TH, true>(t, c, 0);
+            const uint4 x = k < cols ? *(const uint4*)(p + k) : make_uint4(0, 0, 0, 0);
+            w[0] = x.x;
+            w[1] = x.y;
+            w[2] = x.z;
+            w[3] = x.w;
+        } else {
+            w[0] = w[1] = w[2] = w[3] = 0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const uint32_t k = row_col<TH, false>(t, c, j);
+                if (k < cols) w[j >> 1] |= (uint32_t)((const uint16_t*)p)[k] << (j & 1) * 16;
+            }
+        }
+    }
+    __device__ __forceinline__ float get(int j) const { return (float)__builtin_bit_cast(T, (uint16_t)(w[j >> 1] >> (j & 1) * 16)); }
+    /* from here on the values are unpacked anew, not kept */
+    __device__ __forceinline__ void forget() {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(w[i]));
+    }
+};
+template <int TH, bool WIDE>
+struct RawQ {
+    uint32_t w[2];
+    __device__ __forceinline__ void load(const int8_t* p, int t, int c, uint32_t cols) {
+        if (WIDE) {
+            const uint32_t k = row_col<TH, true>(t, c, 0);
+            const uint2 x = k < cols ? *(const uint2*)(p + k) : make_uint2(0, 0);
+            w[0] = x.x;
+            w[1] = x.y;
+        } else {
+            w[0] = w[1] = 0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const uint32_t k = row_col<TH, false>(t, c, j);
+                if (k < cols) w[j >> 2] |= (uint32_t)(uint8_t)p[k] << (j & 3) * 8;
+            }
+        }
+    }
+    __device__ __forceinline__ float get(int j) const { return (float)((int)(w[j >> 2] << (24 - (j & 3) * 8)) >> 24); }
+    __device__ __forceinline__ void forget() {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) asm volatile("" : "+v"(w[i]));
+    }
+};
+
 /* ---- 8-bit checkpoints ------------------------------------------------------------------------------- */
 struct RowArgs {
     const void* src;
@@ -145,11 +229,14 @@ struct RowArgs {
     uint64_t ld_src, ld_dst;
     uint32_t rows, cols;
 };
-/* The largest finite magnitude is scaled by a power of two into [1, 2), and the row with it (exact but for entries below 2^-126 of it,
- * whose q is 0 either way), so that nothing overflows or gets lost.  With a 16-bit significand or less, 127 x is exact in
- * float32; a quotient from the rounded reciprocal is at most one off the nearest whole number, and the remainder 127 x - q amax, exact
- * too (q and amax have 7 and 11 bits), says which way.
- * Rows longer than the registers hold (NCH = 0) are read twice. */
+/* The row is scaled by a power of two so that amax, the largest finite magnitude, lies in [1, 2): nothing overflows or gets lost (but entries
+ * below 2^-126 of amax, whose q is 0 either way).  x and amax have at most 11 significant bits, so t = 127 x has 18 and is exact in
+ * float32, and a quotient t / amax that is not half way between two whole numbers is at least 2^-20 of itself away from that.  One correction of
+ * t (1 / amax) by the exact remainder gives a quotient within 2^-23 of itself, and exactly the quotient where that is half a whole
+ * number: rounding it, half to even, is then rounding t / amax.  Added to 1.5 * 2^23 its low byte is q.
+ * Rows with infinities or NaNs, or an amax out of the range of these scalings, take the careful way: q from the whole number next to the quotient by the
+ * sign of the remainder t - q amax.
+ * Bound by memory: 8192 x 11008 in SPEED_ENCODE.  Rows longer than the registers hold (NCH = 0) are read twice. */
 __device__ __forceinline__ float quantised(float x, float amax, float inv, int e) {
     const float t = 127.0f * ldexpf(x, e);
     float q = rintf(t * inv);
@@ -167,7 +254,7 @@ __device__ __forceinline__ float finite_magnitude(float x) {
 }
 template <class T, bool WIDE, int TH, int NCH>
 __global__ __launch_bounds__(TH < 256 ? 256 : TH) void checkpoint_encode(const RowArgs a) {
-    __shared__ float cells[16];
+    __shared__ float cells[2][16];
     const int t = threadIdx.x % TH;
     constexpr uint32_t SETS = TH < 256 ? 256 / TH : 1;
     const int chunks = NCH ? NCH : (a.cols + TH * 8 - 1) / (TH * 8);
@@ -175,32 +262,63 @@ __global__ __launch_bounds__(TH < 256 ? 256 : TH) void checkpoint_encode(const R
     for (uint64_t row = (uint64_t)blockIdx.x * SETS + threadIdx.x / TH; row < a.rows; row += (uint64_t)gridDim.x * SETS) {
         const T* src = (const T*)a.src + row * a.ld_src;
         int8_t* dst = (int8_t*)a.dst + row * a.ld_dst;
-        float x[NCH ? NCH : 1][8];
-        float m = 0.0f;
+        Raw<T, TH, WIDE> x[NCH ? NCH : 1];
+        /* magnitudes compare like their bits, two at a time */
+        typedef uint16_t s2 __attribute__((ext_vector_type(2)));
+        s2 top = {0, 0};
+#pragma unroll
+        for (int c = 0; c < (NCH ? NCH : 1); ++c) x[c].load(src, t, c, a.cols);
         for (int c = 0; c < chunks; ++c) {
-            float* v = x[NCH ? c : 0];
-            load8<T, TH, WIDE>(src, t, c, a.cols, v);
-            for (int j = 0; j < 8; ++j) m = fmaxf(m, finite_magnitude(v[j]));
+            if (!NCH) x[0].load(src, t, c, a.cols);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) top = __builtin_elementwise_max(top, __builtin_bit_cast(s2, x[NCH ? c : 0].w[i] & 0x7FFF7FFFu));
         }
-        m = group_max<TH>(m, cells, t);
+        float m = fmaxf((float)top[0], (float)top[1]);                                 /* bits as whole numbers, exact */
+        m = group_max<TH>(m, cells[0], t);
+        const uint16_t bits = (uint16_t)m;
+        m = (float)__builtin_bit_cast(T, bits);
+        const bool numbers = m < INFINITY;
+        if (!numbers) {
+            m = 0.0f;
+            for (int c = 0; c < chunks; ++c) {
+                if (!NCH) x[0].load(src, t, c, a.cols);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) m = fmaxf(m, finite_magnitude(x[NCH ? c : 0].get(j)));
+            }
+            m = group_max<TH>(m, cells[1], t);
+        }
         if (t == 0) a.scale[row] = m / 127.0f;
         const int e = m > 0.0f ? -ilogbf(m) : 0;
         const float amax = m > 0.0f ? ldexpf(m, e) : 1.0f, inv = 1.0f / amax;
+        const bool plain = numbers && e > -100 && e < 100;
+        const float times127 = plain ? ldexpf(127.0f, e) : 0.0f, quick = times127 * inv;
         for (int c = 0; c < chunks; ++c) {
-            float* v = x[NCH ? c : 0];
-            if (!NCH) load8<T, TH, WIDE>(src, t, c, a.cols, v);
+            if (!NCH) x[0].load(src, t, c, a.cols);
+            const Raw<T, TH, WIDE>& r = x[NCH ? c : 0];
+            uint32_t q[8];
+            if (plain) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float v = r.get(j), n = v * times127, near = v * quick;
+                    q[j] = __builtin_bit_cast(uint32_t, fmaf(fmaf(-near, amax, n), inv, near) + 12582912.0f);
+                }
+            } else {
+                for (int j = 0; j < 8; ++j) q[j] = (uint32_t)(int)quantised(r.get(j), amax, inv, e);
+            }
             if (WIDE) {
                 const uint32_t k = row_col<TH, true>(t, c, 0);
-                q8 q;
-                for (int j = 0; j < 8; ++j) q[j] = (int8_t)quantised(v[j], amax, inv, e);
-                if (k < a.cols) *(q8*)(dst + k) = q;
+                uint2 w;
+                w.x = __builtin_amdgcn_perm(__builtin_amdgcn_perm(q[3], q[2], 0x0C0C0400u), __builtin_amdgcn_perm(q[1], q[0], 0x0C0C0400u), 0x05040100u);
+                w.y = __builtin_amdgcn_perm(__builtin_amdgcn_perm(q[7], q[6], 0x0C0C0400u), __builtin_amdgcn_perm(q[5], q[4], 0x0C0C0400u), 0x05040100u);
+                if (k < a.cols) *(uint2*)(dst + k) = w;
             } else {
                 for (int j = 0; j < 8; ++j) {
                     const uint32_t k = row_col<TH, false>(t, c, j);
-                    if (k < a.cols) dst[k] = (int8_t)quantised(v[j], amax, inv, e);
+                    if (k < a.cols) dst[k] = (int8_t)q[j];
                 }
             }
         }
+        if (TH > 64) __syncthreads();                    /* the cells are free again */
     }
 }
 /* 256 lanes take 2048 entries of a row */
@@ -228,53 +346,65 @@ struct NormArgs {
 };
 template <class T, bool WIDE, int TH, int NCH>
 __global__ __launch_bounds__(TH < 256 ? 256 : TH) void norm_forward(const NormArgs a) {
-    __shared__ float cells[16];
+    __shared__ float cells[2][16];
     const int t = threadIdx.x % TH;
     constexpr uint32_t SETS = TH < 256 ? 256 / TH : 1;
+    const float per = 1.0f / (float)a.cols;
+    Raw<T, TH, WIDE> g[NCH], b[NCH];                 /* under way while the sums are formed */
+#pragma unroll
+    for (int c = 0; c < NCH; ++c) {
+        if (a.gamma) g[c].load((const T*)a.gamma, t, c, a.cols);
+        if (a.beta) b[c].load((const T*)a.beta, t, c, a.cols);
+    }
     for (uint64_t row = (uint64_t)blockIdx.x * SETS + threadIdx.x / TH; row < a.rows; row += (uint64_t)gridDim.x * SETS) {
         float x[NCH][8];
+#pragma unroll
         for (int c = 0; c < NCH; ++c) {
             if (a.scale) load8q<TH, WIDE>((const int8_t*)a.x + row * a.ldx, a.scale[row], t, c, a.cols, x[c]);
             else load8<T, TH, WIDE>((const T*)a.x + row * a.ldx, t, c, a.cols, x[c]);
         }
-        const float per = 1.0f / (float)a.cols;
         float mean = 0.0f;
         if (a.centred) {
             float s = 0.0f;
+#pragma unroll
             for (int c = 0; c < NCH; ++c)
+#pragma unroll
                 for (int j = 0; j < 8; ++j) s += x[c][j];
-            mean = group_sum<TH>(s, cells, t) * per;
+            mean = group_sum<TH>(s, cells[0], t) * per;
         }
         float s = 0.0f;
+#pragma unroll
         for (int c = 0; c < NCH; ++c)
+#pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const float d = row_col<TH, WIDE>(t, c, j) < a.cols ? x[c][j] - mean : 0.0f;
                 x[c][j] = d;
                 s += d * d;
             }
-        const float rstd = 1.0f / sqrtf(group_sum<TH>(s, cells, t) * per + a.eps);
+        const float rstd = 1.0f / sqrtf(group_sum<TH>(s, cells[1], t) * per + a.eps);
         if (t == 0) {
             if (a.mean) a.mean[row] = mean;
             if (a.rstd) a.rstd[row] = rstd;
         }
+#pragma unroll
         for (int c = 0; c < NCH; ++c) {
-            float g[8], b[8];
-            if (a.gamma) load8<T, TH, WIDE>((const T*)a.gamma, t, c, a.cols, g);
-            if (a.beta) load8<T, TH, WIDE>((const T*)a.beta, t, c, a.cols, b);
+#pragma unroll
             for (int j = 0; j < 8; ++j) {
                 float v = x[c][j] * rstd;
-                if (a.gamma) v *= g[j];
-                if (a.beta) v += b[j];
+                if (a.gamma) v *= g[c].get(j);
+                if (a.beta) v += b[c].get(j);
                 x[c][j] = v;
             }
             store8<T, TH, WIDE>((T*)a.y + row * a.ldy, t, c, a.cols, x[c]);
         }
+        if (TH > 64) __syncthreads();                /* the cells are free again */
     }
 }
 
-/* The gradient: a workgroup of 1024 lanes takes 1024 / TH rows at a time and every gridDim-th such set; a lane keeps the sums of dy xh and dy
+/* The gradient: a workgroup of LANES lanes takes LANES / TH rows at a time and every gridDim-th such set; a lane keeps the sums of dy xh and dy
  * for its columns over all of them, so that gamma's and beta's gradients cost one partial row per workgroup and no second
- * pass over the activations.  The row sets of a workgroup are added in order through LDS; column_sums adds the workgroups. */
+ * pass over the activations.  The next set's loads are under way while this one's two sums are formed, at one barrier a set (the cells
+ * alternate).  The row sets of a workgroup are added in order through LDS; column_sums adds the workgroups. */
 struct NormBackArgs {
     const void *dy, *x;
     const float* scale;
@@ -286,78 +416,123 @@ struct NormBackArgs {
     uint32_t rows, cols;
     int centred;
 };
-static const int NORM_BACK_LANES = 1024;
-template <class T, bool WIDE, int TH, int NCH>
-__global__ __launch_bounds__(NORM_BACK_LANES) void norm_backward(const NormBackArgs a) {
+template <class T, bool EIGHT, bool WIDE, int TH, int NCH, int LANES>
+__global__ __launch_bounds__(LANES) void norm_backward(const NormBackArgs a) {
     extern __shared__ float lds[];
-    constexpr int SETS = NORM_BACK_LANES / TH;
-    __shared__ float cells[2][16];
+    constexpr int SETS = LANES / TH;
+    __shared__ float2 cells[2][16];
     const int t = threadIdx.x % TH, set = threadIdx.x / TH;
-    float *cell0 = cells[0] + set * (TH / 64), *cell1 = cells[1] + set * (TH / 64);
     float dg[NCH][8], db[NCH][8];
+#pragma unroll
     for (int c = 0; c < NCH; ++c)
+#pragma unroll
         for (int j = 0; j < 8; ++j) dg[c][j] = db[c][j] = 0.0f;
+    Raw<T, TH, WIDE> gamma[NCH];
+    if (a.gamma)
+#pragma unroll
+        for (int c = 0; c < NCH; ++c) gamma[c].load((const T*)a.gamma, t, c, a.cols);
     const float per = 1.0f / (float)a.cols;
     const uint64_t step = (uint64_t)gridDim.x * SETS;
-    for (uint64_t first = (uint64_t)blockIdx.x * SETS; first < a.rows; first += step) {      /* the same number of rounds for every lane */
-        const uint64_t row = first + set;
+    /* A row is kept as it was read and unpacked twice, for the sums and for dx: two rows' raw bits take fewer registers than one row's values.
+     * Where a lane has more than one chunk of a row there is no room for the next one. */
+    constexpr bool AHEAD = NCH == 1;
+    typedef typename std::conditional<EIGHT, RawQ<TH, WIDE>, Raw<T, TH, WIDE>>::type RawX;
+    struct Row {
+        RawX x[NCH];
+        Raw<T, TH, WIDE> dy[NCH];
+        float mean, rstd, scale;
+    };
+    auto fetch = [&](Row& to, uint64_t row) {
         const bool live = row < a.rows;
         const uint32_t cols = live ? a.cols : 0;
         const uint64_t r = live ? row : 0;
-        const float mean = a.centred ? a.mean[r] : 0.0f, rstd = a.rstd[r];
-        float xh[NCH][8], g[NCH][8];
-        float sg = 0.0f, sgx = 0.0f;
+#pragma unroll
         for (int c = 0; c < NCH; ++c) {
-            if (a.scale) load8q<TH, WIDE>((const int8_t*)a.x + r * a.ldx, a.scale[r], t, c, cols, xh[c]);
-            else load8<T, TH, WIDE>((const T*)a.x + r * a.ldx, t, c, cols, xh[c]);
-            load8<T, TH, WIDE>((const T*)a.dy + r * a.lddy, t, c, cols, g[c]);
-            float gm[8];
-            if (a.gamma) load8<T, TH, WIDE>((const T*)a.gamma, t, c, a.cols, gm);
-            for (int j = 0; j < 8; ++j) {
-                const bool in = row_col<TH, WIDE>(t, c, j) < cols;
-                const float h = in ? (xh[c][j] - mean) * rstd : 0.0f;
-                const float dy = g[c][j];
-                dg[c][j] += dy * h;
-                db[c][j] += dy;
-                const float gg = a.gamma ? dy * gm[j] : dy;
-                xh[c][j] = h;
-                g[c][j] = gg;
-                sg += gg;
-                sgx += gg * h;
-            }
+            if constexpr (EIGHT) to.x[c].load((const int8_t*)a.x + r * a.ldx, t, c, cols);
+            else to.x[c].load((const T*)a.x + r * a.ldx, t, c, cols);
+            to.dy[c].load((const T*)a.dy + r * a.lddy, t, c, cols);
         }
-        if (a.dx) {
-            sg = group_sum<TH>(sg, cell0, t);
-            sgx = group_sum<TH>(sgx, cell1, t);
-            const float mg = a.centred ? sg * per : 0.0f, mgx = sgx * per;
-            for (int c = 0; c < NCH; ++c) {
-                for (int j = 0; j < 8; ++j) g[c][j] = rstd * (g[c][j] - mg - xh[c][j] * mgx);
-                store8<T, TH, WIDE>((T*)a.dx + r * a.lddx, t, c, cols, g[c]);
+        to.rstd = a.rstd[r];
+        to.mean = a.centred ? a.mean[r] : 0.0f;
+        to.scale = EIGHT ? a.scale[r] : 1.0f;
+    };
+    auto work = [&](Row& now, uint64_t row, float2* cell) {
+        const uint32_t cols = row < a.rows ? a.cols : 0;
+        float sg = 0.0f, sgx = 0.0f;
+#pragma unroll
+        for (int c = 0; c < NCH; ++c)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const bool in = WIDE ? row_col<TH, true>(t, c, 0) < cols : row_col<TH, false>(t, c, j) < cols;
+                const float h = in ? (now.x[c].get(j) * now.scale - now.mean) * now.rstd : 0.0f, d = now.dy[c].get(j);
+                dg[c][j] += d * h;
+                db[c][j] += d;
+                const float g = a.gamma ? d * gamma[c].get(j) : d;
+                sg += g;
+                sgx += g * h;
             }
+        if (!a.dx) return;
+        group_sum2<TH>(sg, sgx, cell, t);
+        const float mg = a.centred ? sg * per : 0.0f, mgx = sgx * per;
+#pragma unroll
+        for (int c = 0; c < NCH; ++c) {
+            now.x[c].forget();
+            now.dy[c].forget();
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float h = (now.x[c].get(j) * now.scale - now.mean) * now.rstd, d = now.dy[c].get(j), g = a.gamma ? d * gamma[c].get(j) : d;
+                v[j] = now.rstd * (g - mg - h * mgx);
+            }
+            store8<T, TH, WIDE>((T*)a.dx + row * a.lddx, t, c, cols, v);
+        }
+    };
+    float2 *cell0 = cells[0] + set * (TH / 64), *cell1 = cells[1] + set * (TH / 64);
+    /* every lane of the workgroup makes the same rounds */
+    const uint64_t begin = (uint64_t)blockIdx.x * SETS;
+    if constexpr (AHEAD) {
+        Row one, two;
+        fetch(one, begin + set);
+        for (uint64_t first = begin; first < a.rows; first += 2 * step) {
+            fetch(two, first + step + set);
+            work(one, first + set, cell0);
+            if (first + step >= a.rows) break;
+            fetch(one, first + 2 * step + set);
+            work(two, first + step + set, cell1);
+        }
+    } else {
+        Row one;
+        int turn = 0;
+        for (uint64_t first = begin; first < a.rows; first += step, turn ^= 1) {
+            fetch(one, first + set);
+            work(one, first + set, turn ? cell1 : cell0);
         }
     }
     if (!a.part) return;
+#pragma unroll
     for (int which = 0; which < 2; ++which) {
         float* part = a.part + ((uint64_t)blockIdx.x * 2 + which) * a.cols;
         for (int s = 0; s < SETS; ++s) {
-            __syncthreads();
-            if (set == s)
-                for (int c = 0; c < NCH; ++c)
-                    for (int j = 0; j < 8; ++j) {
-                        const uint32_t k = row_col<TH, WIDE>(t, c, j);
-                        if (k >= a.cols) continue;
-                        float v = which ? db[c][j] : dg[c][j];
-                        if (s) v += lds[k];
-                        if (s + 1 < SETS) lds[k] = v;
-                        else part[k] = v;
-                    }
+            if (SETS > 1) __syncthreads();
+            if (set != s) continue;
+#pragma unroll
+            for (int c = 0; c < NCH; ++c)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const uint32_t k = row_col<TH, WIDE>(t, c, j);
+                    if (k >= a.cols) continue;
+                    float v = which ? db[c][j] : dg[c][j];
+                    if (s) v += lds[k];
+                    if (s + 1 < SETS) lds[k] = v;
+                    else part[k] = v;
+                }
         }
     }
 }
 /* out[k] = sum over i < n of part[i * stride + k]: 64 columns to a workgroup, 16 waves that take every 16th partial row, joined in order */
 struct ColumnSumArgs {
     const float* part;
-    float* out;
+    float* out[2];                   /* of the second one (blockIdx.y) the partial rows lie cols further on; null: not wanted */
     uint64_t stride;
     uint32_t n, cols;
 };
@@ -365,14 +540,18 @@ __global__ __launch_bounds__(1024) void column_sums(const ColumnSumArgs a) {
     __shared__ float cells[16][64];
     const int w = threadIdx.x / 64, l = threadIdx.x % 64;
     const uint32_t k = blockIdx.x * 64 + l;
+    float* out = a.out[blockIdx.y];
+    if (!out) return;
+    const float* part = a.part + (uint64_t)blockIdx.y * a.cols;
     float s = 0.0f;
     if (k < a.cols)
-        for (uint32_t i = w; i < a.n; i += 16) s += a.part[i * a.stride + k];
+#pragma unroll 4
+        for (uint32_t i = w; i < a.n; i += 16) s += part[i * a.stride + k];
     cells[w][l] = s;
     __syncthreads();
     if (w || k >= a.cols) return;
     for (int i = 1; i < 16; ++i) s += cells[i][l];
-    a.out[k] = s;
+    out[k] = s;
 }
 
 /* ---- products ------------------------------------------------------------------------------------------
@@ -477,50 +656,64 @@ __device__ __forceinline__ void put8(void* base, uint64_t ld, uint32_t q, uint32
             if (p + i < np) at[i] = (T)v[i];
     }
 }
-template <class T>
-__device__ __forceinline__ void get8(const void* base, uint64_t ld, uint32_t q, uint32_t p, uint32_t np, bool whole, float* v) {
-    const T* at = (const T*)base + q * ld + p;
-    if (whole) {
-        const typename Vec<T>::v8 x = *(const typename Vec<T>::v8*)at;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = (float)x[i];
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = p + i < np ? (float)at[i] : 0.0f;
-    }
-}
+/* The epilogue of eight entries of column p on.  What it needs for the columns is loaded once, by the constructor; what it needs for the entries,
+ * the residual, by ask(), ahead of apply(). */
 template <class T, bool FORWARD>
-__device__ __forceinline__ void finish8(const ProductArgs& a, uint32_t q, uint32_t p, float* v) {
-    if (q >= a.nq || p >= a.np) return;
-    const bool whole = a.wide_out;
-    if (FORWARD) {
-        float r[8];
+struct Finish {
+    const ProductArgs& a;
+    const uint32_t p;
+    float scale[8], bias[8];
+    typename Vec<T>::v8 res;
+    __device__ __forceinline__ Finish(const ProductArgs& a_, uint32_t p_) : a(a_), p(p_) {
+        if (!FORWARD) {
+            scale[0] = a.factor ? a.factor[0] : 1.0f;
+            return;
+        }
         if (a.p_scale) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] *= p + i < a.np ? a.p_scale[p + i] : 0.0f;
+            for (int i = 0; i < 8; ++i) scale[i] = p + i < a.np ? a.p_scale[p + i] : 0.0f;
         }
         if (a.bias) {
-            get8<T>(a.bias, 0, 0, p, a.np, whole, r);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] += r[i];
+            for (int i = 0; i < 8; ++i) bias[i] = p + i < a.np ? (float)((const T*)a.bias)[p + i] : 0.0f;
         }
-        if (a.z) put8<T>(a.z, a.ldz, q, p, a.np, whole, v);
-        if (a.act != TC_ACT_NONE) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = activate(v[i], a.act);
-        }
-        if (a.residual) {
-            get8<T>(a.residual, a.ldres, q, p, a.np, whole, r);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] += r[i];
-        }
-    } else if (a.factor) {
-        const float f = a.factor[0];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] *= f;
     }
-    put8<T>(a.out, a.ldo, q, p, a.np, whole, v);
-}
+    __device__ __forceinline__ void ask(uint32_t q) {
+        if (!FORWARD || !a.residual || q >= a.nq || p >= a.np) return;
+        const T* at = (const T*)a.residual + q * a.ldres + p;
+        if (a.wide_out) res = *(const typename Vec<T>::v8*)at;
+        else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) res[i] = p + i < a.np ? at[i] : (T)0.0f;
+        }
+    }
+    __device__ __forceinline__ void apply(uint32_t q, float* v) const {
+        if (q >= a.nq || p >= a.np) return;
+        if (FORWARD) {
+            if (a.p_scale) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] *= scale[i];
+            }
+            if (a.bias) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] += bias[i];
+            }
+            if (a.z) put8<T>(a.z, a.ldz, q, p, a.np, a.wide_out, v);
+            if (a.act != TC_ACT_NONE) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = activate(v[i], a.act);
+            }
+            if (a.residual) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] += (float)res[i];
+            }
+        } else if (a.factor) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] *= scale[0];
+        }
+        put8<T>(a.out, a.ldo, q, p, a.np, a.wide_out, v);
+    }
+};
 /* A wave's NP x NQ blocks of sixteen by sixteen, through a piece of LDS of its own (NP * 16 + 4 floats for each of sixteen q): a lane of
  * the matrix instruction holds four entries of a row, and memory wants whole lines.  The workgroup must have passed a barrier since
  * LDS was last read otherwise. */
@@ -529,16 +722,19 @@ template <class T, bool FORWARD, int NP, int NQ>
 __device__ __forceinline__ void drain(const ProductArgs& a, f4 (&acc)[NP][NQ], uint8_t* lds, uint32_t q0, uint32_t p0, uint32_t split, int lane) {
     float* buf = (float*)lds;
     constexpr int LD = NP * 16 + 4, GROUPS = NP * 2, ROWS = 64 / GROUPS;
+    const uint32_t p = p0 + (lane % GROUPS) * 8, row = lane / GROUPS;
+    Finish<T, FORWARD> end(a, p);
+    end.ask(q0 + row);
 #pragma unroll
     for (int j = 0; j < NQ; ++j) {
 #pragma unroll
         for (int i = 0; i < NP; ++i) *(f4*)(buf + (lane & 15) * LD + i * 16 + (lane >> 4) * 4) = acc[i][j];
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");        /* lanes read what others of the wave have written */
 #pragma unroll 1
-        for (int r = lane / GROUPS; r < 16; r += ROWS) {
+        for (int r = row; r < 16; r += ROWS) {
             const float* at = buf + r * LD + (lane % GROUPS) * 8;
             const f4 lo = *(const f4*)at, hi = *(const f4*)(at + 4);
-            const uint32_t q = q0 + j * 16 + r, p = p0 + (lane % GROUPS) * 8;
+            const uint32_t q = q0 + j * 16 + r;
             if (a.part) {
                 if (q < a.nq && p < a.np) {
                     f4* to = (f4*)(a.part + (split * (uint64_t)a.nq + q) * a.ldp + p);
@@ -547,7 +743,9 @@ __device__ __forceinline__ void drain(const ProductArgs& a, f4 (&acc)[NP][NQ], u
                 }
             } else {
                 float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-                finish8<T, FORWARD>(a, q, p, v);
+                Finish<T, FORWARD> now = end;
+                end.ask(q + ROWS);                       /* rows of this block, then of the next, are ROWS apart */
+                now.apply(q, v);
             }
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -815,14 +1013,17 @@ __global__ __launch_bounds__(256) void join_parts(const ProductArgs a, uint32_t 
     const uint64_t n = (uint64_t)blockIdx.x * 256 + threadIdx.x;
     if (n >= (uint64_t)per * a.nq) return;
     const uint32_t q = (uint32_t)(n / per), p = (uint32_t)(n % per) * 8;
+    Finish<T, FORWARD> end(a, p);
+    end.ask(q);
     f4 lo = {0, 0, 0, 0}, hi = {0, 0, 0, 0};
+#pragma unroll 4
     for (uint32_t i = 0; i < splits; ++i) {
         const f4* at = (const f4*)(a.part + (i * (uint64_t)a.nq + q) * a.ldp + p);
         lo += at[0];
         hi += at[1];
     }
     float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-    finish8<T, FORWARD>(a, q, p, v);
+    end.apply(q, v);
 }
 
 /* ---- a few rows -------------------------------------------------------------------------------------------------
@@ -846,30 +1047,43 @@ __global__ __launch_bounds__(WAVES * 64) void product_thin(const ProductArgs a) 
     constexpr int AHEAD = EIGHT ? 8 : 4;
     const uint32_t chunks = (a.nr + 63) / 64;
     for (uint32_t c = w; c < chunks; c += WAVES * AHEAD) {
-        u4 x[AHEAD][EIGHT ? 1 : 2], y[AHEAD][2];
-#pragma unroll
-        for (int i = 0; i < AHEAD; ++i) {
+        u4 x[AHEAD][EIGHT ? 1 : 2];
+        auto place = [&](int i, uint32_t off, uint32_t& from) {
             const uint32_t r = (c + i * WAVES) * 64;
-            const bool in = r + at < a.nr;
-            const uint32_t fp = in ? op : NOWHERE, fq = in ? oq : NOWHERE;
-            const uint32_t sp = in || c + i * WAVES < chunks ? r * SIZE : 0, sq = c + i * WAVES < chunks ? r * 2 : 0;
-            x[i][0] = __builtin_amdgcn_raw_buffer_load_b128(rp, fp, sp, 0);
-            if (!EIGHT) x[i][EIGHT ? 0 : 1] = __builtin_amdgcn_raw_buffer_load_b128(rp, fp == NOWHERE ? NOWHERE : fp + 16, sp, 0);
-            y[i][0] = __builtin_amdgcn_raw_buffer_load_b128(rq, fq, sq, 0);
-            y[i][1] = __builtin_amdgcn_raw_buffer_load_b128(rq, fq == NOWHERE ? NOWHERE : fq + 16, sq, 0);
-        }
+            from = r < a.nr ? r : 0;
+            return r + at < a.nr ? off : NOWHERE;
+        };
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
-            v8 lo, hi;
-            if (EIGHT) {
-                lo = widen<T>(x[i][0][0], x[i][0][1]);
-                hi = widen<T>(x[i][0][2], x[i][0][3]);
-            } else {
-                lo = __builtin_bit_cast(v8, x[i][0]);
-                hi = __builtin_bit_cast(v8, x[i][EIGHT ? 0 : 1]);
+            uint32_t from;
+            const uint32_t o = place(i, op, from);
+            x[i][0] = __builtin_amdgcn_raw_buffer_load_b128(rp, o, from * SIZE, 0);
+            if constexpr (!EIGHT) x[i][1] = __builtin_amdgcn_raw_buffer_load_b128(rp, o == NOWHERE ? NOWHERE : o + 16, from * SIZE, 0);
+        }
+        /* the rows of x come from the caches, two chunks at a time */
+#pragma unroll
+        for (int i = 0; i < AHEAD; i += 2) {
+            u4 y[2][2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                uint32_t from;
+                const uint32_t o = place(i + k, oq, from);
+                y[k][0] = __builtin_amdgcn_raw_buffer_load_b128(rq, o, from * 2, 0);
+                y[k][1] = __builtin_amdgcn_raw_buffer_load_b128(rq, o == NOWHERE ? NOWHERE : o + 16, from * 2, 0);
             }
-            acc = mfma<T>(lo, __builtin_bit_cast(v8, y[i][0]), acc);
-            acc = mfma<T>(hi, __builtin_bit_cast(v8, y[i][1]), acc);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                v8 lo, hi;
+                if constexpr (EIGHT) {
+                    lo = widen<T>(x[i + k][0][0], x[i + k][0][1]);
+                    hi = widen<T>(x[i + k][0][2], x[i + k][0][3]);
+                } else {
+                    lo = __builtin_bit_cast(v8, x[i + k][0]);
+                    hi = __builtin_bit_cast(v8, x[i + k][1]);
+                }
+                acc = mfma<T>(lo, __builtin_bit_cast(v8, y[k][0]), acc);
+                acc = mfma<T>(hi, __builtin_bit_cast(v8, y[k][1]), acc);
+            }
         }
     }
     /* acc: q = lane & 15, p from 4 (lane >> 4) on */
@@ -878,26 +1092,29 @@ __global__ __launch_bounds__(WAVES * 64) void product_thin(const ProductArgs a) 
     __syncthreads();
     if (t >= 32) return;
     const uint32_t q = t >> 1, p = (t & 1) * 8;
+    Finish<T, true> end(a, p0 + p);
+    end.ask(q);
     float v[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         v[i] = sums[0][q * 16 + p + i];
         for (int k = 1; k < WAVES; ++k) v[i] += sums[k][q * 16 + p + i];
     }
-    finish8<T, true>(a, q, p0 + p, v);
+    end.apply(q, v);
 }
 
 /* ---- the gradient before the activation ------------------------------------------------------------------
  * dz = dy act'(z), and its sums over the rows.  int8 operands of the products that follow have a scale for each of the
  * rows that those products sum over; it is put into their other operand here, from the unrounded value: by_x = dz s_x[row] / m_x for dw,
  * by_w = dz s_w[column] / m_w for dx.  So whole numbers enter the matrix instruction exactly and one rounding of the
- * gradient is all there is.  m is the power of two above the largest scale: it keeps float16 in its range and is put back, exactly, after the product. */
+ * gradient is all there is.  m is the power of two above the largest scale: it keeps float16 in its range and is put back, exactly, after the product (bfloat16 has
+ * float32's range and takes m = 1). */
 struct SlopeArgs {
     const void *dy, *z;
     const float* z_scale;            /* z is int8 where this is set */
     void *dz, *by_x, *by_w;
     const float *x_scale, *w_scale;
-    const float* m;                  /* m_x, 1 / m_x, m_w, 1 / m_w */
+    const float* m;                  /* m_x, 1 / m_x, m_w, 1 / m_w; null: ones */
     float* part;                     /* [gridDim.y][cols] */
     uint64_t lddy, ldz, lddz;        /* by_x, by_w: cols side by side, padded to ld_by */
     uint64_t ld_by;
@@ -909,6 +1126,7 @@ __global__ __launch_bounds__(1024) void scale_peak(const float* x, uint32_t nx, 
     const float* s = blockIdx.x ? w : x;
     const uint32_t n = s ? (blockIdx.x ? nw : nx) : 0;
     float v = 0.0f;
+#pragma unroll 8
     for (uint32_t i = threadIdx.x; i < n; i += 1024) v = fmaxf(v, finite_magnitude(s[i]));
     v = group_max<1024>(v, cells, threadIdx.x);
     if (threadIdx.x) return;
@@ -925,7 +1143,7 @@ __global__ __launch_bounds__(256) void slopes(const SlopeArgs a) {
     const uint32_t c0 = blockIdx.x * 512;
     const uint32_t cols = a.cols - c0 < 512 ? a.cols - c0 : 512;
     float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0}, ws[8];
-    const float mx = a.by_x ? a.m[1] : 0.0f, mw = a.by_w ? a.m[3] : 0.0f;
+    const float mx = a.by_x && a.m ? a.m[1] : 1.0f, mw = a.by_w && a.m ? a.m[3] : 1.0f;
     if (a.by_w)
         for (int j = 0; j < 8; ++j) {
             const uint32_t k = row_col<64, WIDE>(t, 0, j);

@@ -6,6 +6,7 @@
  */
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "ctx.h"
 #if defined(TC_HOST_EMU)
@@ -63,10 +64,13 @@ int check_workspace(tc_ctx* ctx, const void* ws, size_t have, size_t need) {
 size_t up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 /* rows of the input gradient that one workgroup of its kernel has in flight */
-uint32_t norm_back_sets(uint32_t cols) { return cols <= 512 ? 16 : cols <= 4096 ? 4 : 1; }
+uint32_t norm_back_sets(uint32_t rows, uint32_t cols) {
+    if (rows < 1024) return cols <= 512 ? 4 : 1;
+    return cols <= 512 ? 16 : cols <= 2048 ? 4 : cols <= 4096 ? 2 : 1;
+}
 /* workgroups of it: one for each compute unit, each leaves a partial row of gamma's and beta's gradients */
 uint32_t norm_back_groups(uint32_t rows, uint32_t cols) {
-    const uint32_t sets = norm_back_sets(cols);
+    const uint32_t sets = norm_back_sets(rows, cols);
     return std::min<uint32_t>(256, (rows + sets - 1) / sets);
 }
 /* sets of rows over which the gradient before the activation is spread: about eight workgroups for each compute unit */
@@ -94,7 +98,7 @@ ProductPlan product_plan(uint32_t np, uint32_t nq, uint32_t nr) {
         uint32_t side, deepest;
         double step[5];
     };
-    static const Layout layouts[3] = {{256, 1, {1.8}}, {128, 2, {0.75, 0.97}}, {64, 5, {0.48, 0.5, 0.62, 0.75, 0.9}}};
+    static const Layout layouts[3] = {{256, 1, {1.7}}, {128, 2, {0.75, 0.97}}, {64, 5, {0.48, 0.5, 0.62, 0.75, 0.9}}};
     static const uint32_t parts[] = {1, 2, 3, 4, 6, 8, 12, 16};
     ProductPlan best = {np, nq, 64, 64, 1, nr, up(np, 8)};
     if (!nq || !nr) return best;                     /* no rows: nothing is launched */
@@ -182,22 +186,30 @@ int norm_rows(tc_ctx* ctx, const NormArgs& a) {
     else LAUNCH((norm_forward<T, WIDE, 1024, 4>), row_grid(a.rows), 1024, 0, a);
     return TC_OK;
 }
-template <class T, bool WIDE>
+template <class T, bool EIGHT, bool WIDE>
 int norm_back_rows(tc_ctx* ctx, const NormBackArgs& a, uint32_t groups) {
-    const uint32_t c = a.cols;
-    const dim3 grid(groups);
-    const size_t lds = norm_back_sets(c) > 1 ? (size_t)c * 4 : 0;
-    if (c <= 512) LAUNCH((norm_backward<T, WIDE, 64, 1>), grid, NORM_BACK_LANES, lds, a);
-    else if (c <= 2048) LAUNCH((norm_backward<T, WIDE, 256, 1>), grid, NORM_BACK_LANES, lds, a);
-    else if (c <= 4096) LAUNCH((norm_backward<T, WIDE, 256, 2>), grid, NORM_BACK_LANES, lds, a);
-    else if (c <= 8192) LAUNCH((norm_backward<T, WIDE, 1024, 1>), grid, NORM_BACK_LANES, lds, a);
-    else if (c <= 16384) LAUNCH((norm_backward<T, WIDE, 1024, 2>), grid, NORM_BACK_LANES, lds, a);
-    else LAUNCH((norm_backward<T, WIDE, 1024, 4>), grid, NORM_BACK_LANES, lds, a);
+    const uint32_t c = a.cols, sets = norm_back_sets(a.rows, c);
+    const size_t lds = sets > 1 ? (size_t)c * 4 : 0;
+    if (a.rows < 1024) {                             /* few rows: smaller workgroups, so that they go to more compute units */
+        if (c <= 512) LAUNCH((norm_backward<T, EIGHT, WIDE, 64, 1, 256>), groups, 256, lds, a);
+        else if (c <= 2048) LAUNCH((norm_backward<T, EIGHT, WIDE, 256, 1, 256>), groups, 256, lds, a);
+        else if (c <= 4096) LAUNCH((norm_backward<T, EIGHT, WIDE, 512, 1, 512>), groups, 512, lds, a);
+        else if (c <= 8192) LAUNCH((norm_backward<T, EIGHT, WIDE, 1024, 1, 1024>), groups, 1024, lds, a);
+        else if (c <= 16384) LAUNCH((norm_backward<T, EIGHT, WIDE, 1024, 2, 1024>), groups, 1024, lds, a);
+        else LAUNCH((norm_backward<T, EIGHT, WIDE, 1024, 4, 1024>), groups, 1024, lds, a);
+    } else {
+        if (c <= 512) LAUNCH((norm_backward<T, EIGHT, WIDE, 64, 1, 1024>), groups, 1024, lds, a);
+        else if (c <= 2048) LAUNCH((norm_backward<T, EIGHT, WIDE, 256, 1, 1024>), groups, 1024, lds, a);
+        else if (c <= 4096) LAUNCH((norm_backward<T, EIGHT, WIDE, 512, 1, 1024>), groups, 1024, lds, a);
+        else if (c <= 8192) LAUNCH((norm_backward<T, EIGHT, WIDE, 1024, 1, 1024>), groups, 1024, lds, a);
+        else if (c <= 16384) LAUNCH((norm_backward<T, EIGHT, WIDE, 1024, 2, 1024>), groups, 1024, lds, a);
+        else LAUNCH((norm_backward<T, EIGHT, WIDE, 1024, 4, 1024>), groups, 1024, lds, a);
+    }
     return TC_OK;
 }
-int sum_columns(tc_ctx* ctx, const float* part, uint64_t stride, uint32_t n, uint32_t cols, float* out) {
-    const ColumnSumArgs a{part, out, stride, n, cols};
-    LAUNCH(column_sums, dim3((cols + 63) / 64), 1024, 0, a);
+int sum_columns(tc_ctx* ctx, const float* part, uint64_t stride, uint32_t n, uint32_t cols, float* out, float* second) {
+    const ColumnSumArgs a{part, {out, second}, stride, n, cols};
+    LAUNCH(column_sums, dim3((cols + 63) / 64, second ? 2 : 1), 1024, 0, a);
     return TC_OK;
 }
 template <class T>
@@ -227,7 +239,10 @@ int launch_product(tc_ctx* ctx, K* kernel, const ProductArgs& a, uint64_t grid, 
 template <class T, bool P_ALONG, bool P_EIGHT, bool Q_ALONG, bool FORWARD>
 int multiply(tc_ctx* ctx, ProductArgs a, float* part) {
     const bool pieces = in_pieces(a.p, P_ALONG ? a.nr : a.np, P_EIGHT) && in_pieces(a.q, Q_ALONG ? a.nr : a.nq, false);
-    if (FORWARD && a.nq <= 16 && pieces && in_pieces(a.p, a.nr, P_EIGHT, true) && in_pieces(a.q, a.nr, false, true))
+    /* Up to sixteen rows: a pass over the weights alone, 1 x 4096 -> 4096 in 6.9 us against 10.5 by tiles.  Every workgroup reads all of x, though:
+     * beyond eight rows, 16-bit weights that are past the caches' help go by tiles (16 x 4096 -> 11008: 18.4 us against 25.0). */
+    const bool few = a.nq <= 8 || (a.nq <= 16 && (P_EIGHT || (uint64_t)a.np * a.nr <= 1u << 25));
+    if (FORWARD && few && pieces && in_pieces(a.p, a.nr, P_EIGHT, true) && in_pieces(a.q, a.nr, false, true))
         return launch_product(ctx, product_thin<T, P_EIGHT, 8>, a, (a.np + 15) / 16, 512, 0);
     const ProductPlan plan = product_plan(a.np, a.nq, a.nr);
     if (!pieces) return launch_product(ctx, product<T, P_ALONG, P_EIGHT, Q_ALONG, FORWARD>, a, plan.tiles(128, 128), 256, 0);
@@ -291,10 +306,9 @@ int run_norm_backward(tc_ctx* ctx, int kind, const tc_matrix* dy, const tc_matri
     const NormBackArgs a{dy->d_data, x->d_data, x->dtype == TC_I8 ? x->d_scale : nullptr, gamma, mean, rstd, dx ? dx->d_data : nullptr, part,
                          dy->ld, x->ld, dx ? dx->ld : 0, dy->rows, dy->cols, kind == TC_NORM_LAYER};
     const bool w = wide(dy) && wide(x) && (!dx || wide(dx)) && ((uintptr_t)gamma & 15u) == 0;
-    TRY((w ? norm_back_rows<T, true>(ctx, a, groups) : norm_back_rows<T, false>(ctx, a, groups)));
-    if (dgamma) TRY(sum_columns(ctx, part, 2 * (uint64_t)dy->cols, groups, dy->cols, dgamma));
-    if (dbeta) TRY(sum_columns(ctx, part + dy->cols, 2 * (uint64_t)dy->cols, groups, dy->cols, dbeta));
-    return TC_OK;
+    if (a.scale) TRY((w ? norm_back_rows<T, true, true>(ctx, a, groups) : norm_back_rows<T, true, false>(ctx, a, groups)));
+    else TRY((w ? norm_back_rows<T, false, true>(ctx, a, groups) : norm_back_rows<T, false, false>(ctx, a, groups)));
+    return part ? sum_columns(ctx, part, 2 * (uint64_t)dy->cols, groups, dy->cols, dgamma, dbeta) : TC_OK;
 }
 template <class T>
 int run_linear(tc_ctx* ctx, const tc_matrix* x, const tc_matrix* w, const void* bias, int act, const tc_matrix* residual, const tc_matrix* y, const tc_matrix* z,
@@ -321,9 +335,10 @@ int run_linear_backward(tc_ctx* ctx, const tc_matrix* dy, const tc_matrix* x, co
     const uint32_t rows = dy->rows, out = dy->cols;
     const BackPlan plan = back_plan(rows, dx ? dx->cols : dw ? dw->cols : 0, out);
     uint8_t* base = (uint8_t*)ws;
-    float *m = (float*)(base + plan.m), *parts = (float*)(base + plan.split);
+    /* powers of two beside the scales, which bfloat16 can do without */
+    float *m = std::is_same<T, _Float16>::value ? (float*)(base + plan.m) : nullptr, *parts = (float*)(base + plan.split);
     const bool by_x = dw && x->dtype == TC_I8, by_w = dx && w->dtype == TC_I8;
-    if (by_x || by_w) {
+    if (m && (by_x || by_w)) {
         hipLaunchKernelGGL(scale_peak, dim3(2), dim3(1024), 0, ctx_stream(ctx), by_x ? x->d_scale : nullptr, rows, by_w ? w->d_scale : nullptr, out, m);
         int e = (int)hipGetLastError();
         if (e) return ctx_fail_hip(ctx, e, "launch of scale_peak");
@@ -355,7 +370,7 @@ int run_linear_backward(tc_ctx* ctx, const tc_matrix* dy, const tc_matrix* x, co
         const dim3 grid((out + 511) / 512, groups);
         if (wd) LAUNCH((slopes<T, true>), grid, 256, 0, s);
         else LAUNCH((slopes<T, false>), grid, 256, 0, s);
-        if (dbias) TRY(sum_columns(ctx, s.part, out, groups, out, dbias));
+        if (dbias) TRY(sum_columns(ctx, s.part, out, groups, out, dbias, nullptr));
     }
     const Operand plain = act == TC_ACT_NONE ? Operand{dy->d_data, dy->ld} : Operand{dz->d_data, dz->ld};
     if (dx) {
@@ -368,7 +383,7 @@ int run_linear_backward(tc_ctx* ctx, const tc_matrix* dy, const tc_matrix* x, co
         a.out = dx->d_data;
         a.ldo = dx->ld;
         a.wide_out = wide(dx);
-        a.factor = by_w ? m + 2 : nullptr;
+        a.factor = by_w && m ? m + 2 : nullptr;
         TRY((by_w ? multiply<T, false, true, true, false>(ctx, a, parts) : multiply<T, false, false, true, false>(ctx, a, parts)));
     }
     if (dw) {
