@@ -118,76 +118,97 @@ __device__ __forceinline__ void group_sum2(float& u, float& v, float2* cells, in
 }
 
 /* ---- rows in registers -------------------------------------------------------------------------------
- * TH lanes hold a row of at most TH * 8 * NCH entries, 8 NCH to a lane.  WIDE: lane t's chunk c is the eight entries from (c TH + t) 8
- * on, one 16-byte access (8 bytes of int8); rows that are not so aligned: entry (8 c + j) TH + t, so that the lanes of a
- * wave still read side by side. */
-template <int TH, bool WIDE>
-__device__ __forceinline__ uint32_t row_col(int t, int c, int j) {
-    return WIDE ? ((uint32_t)c * TH + t) * 8 + j : ((uint32_t)c * 8 + j) * TH + t;
+ * TH lanes hold a row of at most TH * 8 * NCH entries, 8 NCH to a lane: lane t's chunk c is the eight entries from (c TH + t) 8 on, one
+ * access of 16 bytes (8 bytes of int8), at any address that is aligned to an entry.  Rows are kept as they were read and unpacked when used. */
+template <class V>
+__device__ __forceinline__ V unaligned(const void* p) {
+    V v;
+    __builtin_memcpy(&v, p, sizeof v);
+    return v;
 }
-template <class T, int TH, bool WIDE>
-__device__ __forceinline__ void load8(const T* p, int t, int c, uint32_t cols, float* v) {
-    if (WIDE) {
-        const uint32_t k = row_col<TH, true>(t, c, 0);
-        typename Vec<T>::v8 x = {0, 0, 0, 0, 0, 0, 0, 0};
-        if (k < cols) x = *(const typename Vec<T>::v8*)(p + k);
-        for (int j = 0; j < 8; ++j) v[j] = (float)x[j];
-    } else {
-        for (int j = 0; j < 8; ++j) {
-            const uint32_t k = row_col<TH, false>(t, c, j);
-            v[j] = k < cols ? (float)p[k] : 0.0f;
-        }
+/* Eight entries of which only the last `count` are wanted, moved to the front, zeros behind them.  The last piece of a row is read as
+ * the row's last eight entries (which are all there) and moved so. */
+__device__ __forceinline__ void to_front(uint32_t (&w)[4], uint32_t count) {
+    const uint32_t n = 8 - count;
+    if (n & 4) {
+        w[0] = w[2];
+        w[1] = w[3];
+        w[2] = w[3] = 0;
+    }
+    if (n & 2) {
+        w[0] = w[1];
+        w[1] = w[2];
+        w[2] = w[3];
+        w[3] = 0;
+    }
+    if (n & 1) {
+#pragma unroll
+        for (int i = 0; i < 3; ++i) w[i] = w[i] >> 16 | w[i + 1] << 16;
+        w[3] >>= 16;
     }
 }
-template <int TH, bool WIDE>
-__device__ __forceinline__ void load8q(const int8_t* p, float scale, int t, int c, uint32_t cols, float* v) {
-    if (WIDE) {
-        const uint32_t k = row_col<TH, true>(t, c, 0);
-        q8 x = {0, 0, 0, 0, 0, 0, 0, 0};
-        if (k < cols) x = *(const q8*)(p + k);
-        for (int j = 0; j < 8; ++j) v[j] = scale * (float)x[j];
-    } else {
-        for (int j = 0; j < 8; ++j) {
-            const uint32_t k = row_col<TH, false>(t, c, j);
-            v[j] = k < cols ? scale * (float)p[k] : 0.0f;
-        }
+__device__ __forceinline__ void to_front(uint32_t (&w)[2], uint32_t count) {
+    const uint32_t n = 8 - count, s = (n & 3) * 8;
+    if (n & 4) {
+        w[0] = w[1];
+        w[1] = 0;
+    }
+    w[0] = __builtin_amdgcn_alignbit(w[1], w[0], s);
+    w[1] >>= s;
+}
+/* the eight entries from p on, of which `count` (up to 8) belong to the row and the rest is to be moved away by to_front; SHORT: read one by one, as the row may have fewer than eight */
+template <bool SHORT>
+__device__ __forceinline__ void read_piece(const uint16_t* p, uint32_t count, uint32_t (&w)[4]) {
+    w[0] = w[1] = w[2] = w[3] = 0;
+    if (SHORT) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if ((uint32_t)j < count) w[j >> 1] |= (uint32_t)p[j] << (j & 1) * 16;
+    } else if (count) {
+        const uint4 x = unaligned<uint4>(p + (int)count - 8);
+        w[0] = x.x;
+        w[1] = x.y;
+        w[2] = x.z;
+        w[3] = x.w;
     }
 }
-template <class T, int TH, bool WIDE>
-__device__ __forceinline__ void store8(T* p, int t, int c, uint32_t cols, const float* v) {
-    if (WIDE) {
-        const uint32_t k = row_col<TH, true>(t, c, 0);
-        typename Vec<T>::v8 x;
-        for (int j = 0; j < 8; ++j) x[j] = (T)v[j];
-        if (k < cols) *(typename Vec<T>::v8*)(p + k) = x;
-    } else {
-        for (int j = 0; j < 8; ++j) {
-            const uint32_t k = row_col<TH, false>(t, c, j);
-            if (k < cols) p[k] = (T)v[j];
-        }
+template <bool SHORT>
+__device__ __forceinline__ void read_piece(const uint8_t* p, uint32_t count, uint32_t (&w)[2]) {
+    w[0] = w[1] = 0;
+    if (SHORT) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if ((uint32_t)j < count) w[j >> 2] |= (uint32_t)p[j] << (j & 3) * 8;
+    } else if (count) {
+        const uint2 x = unaligned<uint2>(p + (int)count - 8);
+        w[0] = x.x;
+        w[1] = x.y;
     }
 }
-
-/* the same in two steps, so that several loads can be under way: raw bits, then values */
-template <class T, int TH, bool WIDE>
+template <int TH>
+__device__ __forceinline__ uint32_t row_col(int t, int c) { return ((uint32_t)c * TH + t) * 8; }
+__device__ __forceinline__ uint32_t entries_at(uint32_t k, uint32_t cols) { return k >= cols ? 0 : cols - k < 8 ? cols - k : 8; }
+template <class T, int TH, bool SHORT>
 struct Raw {
     uint32_t w[4];
     __device__ __forceinline__ void load(const T* p, int t, int c, uint32_t cols) {
-        if (WIDE) {
-            const uint32_t k = row_col<TH, true>(t, c, 0);
-            const uint4 x = k < cols ? *(const uint4*)(p + k) : make_uint4(0, 0, 0, 0);
-            w[0] = x.x;
-            w[1] = x.y;
-            w[2] = x.z;
-            w[3] = x.w;
-        } else {
-            w[0] = w[1] = w[2] = w[3] = 0;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const uint32_t k = row_col<TH, false>(t, c, j);
-                if (k < cols) w[j >> 1] |= (uint32_t)((const uint16_t*)p)[k] << (j & 1) * 16;
-            }
+        const uint32_t k = row_col<TH>(t, c);
+        if (SHORT) {
+            read_piece<true>((const uint16_t*)p + k, entries_at(k, cols), w);
+            return;
         }
+        uint4 x = make_uint4(0, 0, 0, 0);
+        if (k < cols) x = unaligned<uint4>(p + (k + 8 <= cols ? k : cols - 8));
+        w[0] = x.x;
+        w[1] = x.y;
+        w[2] = x.z;
+        w[3] = x.w;
+    }
+    /* once all loads are under way: the last piece of a row that is no whole number of pieces */
+    __device__ __forceinline__ void trim(int t, int c, uint32_t cols) {
+        if (SHORT || (cols & 7) == 0) return;
+        const uint32_t count = entries_at(row_col<TH>(t, c), cols);
+        if (count && count < 8) to_front(w, count);
     }
     __device__ __forceinline__ float get(int j) const { return (float)__builtin_bit_cast(T, (uint16_t)(w[j >> 1] >> (j & 1) * 16)); }
     /* from here on the values are unpacked anew, not kept */
@@ -196,23 +217,25 @@ struct Raw {
         for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(w[i]));
     }
 };
-template <int TH, bool WIDE>
+template <int TH, bool SHORT>
 struct RawQ {
     uint32_t w[2];
     __device__ __forceinline__ void load(const int8_t* p, int t, int c, uint32_t cols) {
-        if (WIDE) {
-            const uint32_t k = row_col<TH, true>(t, c, 0);
-            const uint2 x = k < cols ? *(const uint2*)(p + k) : make_uint2(0, 0);
-            w[0] = x.x;
-            w[1] = x.y;
-        } else {
-            w[0] = w[1] = 0;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const uint32_t k = row_col<TH, false>(t, c, j);
-                if (k < cols) w[j >> 2] |= (uint32_t)(uint8_t)p[k] << (j & 3) * 8;
-            }
+        const uint32_t k = row_col<TH>(t, c);
+        if (SHORT) {
+            read_piece<true>((const uint8_t*)p + k, entries_at(k, cols), w);
+            return;
         }
+        uint2 x = make_uint2(0, 0);
+        if (k < cols) x = unaligned<uint2>(p + (k + 8 <= cols ? k : cols - 8));
+        w[0] = x.x;
+        w[1] = x.y;
+    }
+    /* once all loads are under way: the last piece of a row that is no whole number of pieces */
+    __device__ __forceinline__ void trim(int t, int c, uint32_t cols) {
+        if (SHORT || (cols & 7) == 0) return;
+        const uint32_t count = entries_at(row_col<TH>(t, c), cols);
+        if (count && count < 8) to_front(w, count);
     }
     __device__ __forceinline__ float get(int j) const { return (float)((int)(w[j >> 2] << (24 - (j & 3) * 8)) >> 24); }
     __device__ __forceinline__ void forget() {
@@ -220,6 +243,36 @@ struct RawQ {
         for (int i = 0; i < 2; ++i) asm volatile("" : "+v"(w[i]));
     }
 };
+template <class T, int TH, bool SHORT>
+__device__ __forceinline__ void load8(const T* p, int t, int c, uint32_t cols, float* v) {
+    Raw<T, TH, SHORT> r;
+    r.load(p, t, c, cols);
+    r.trim(t, c, cols);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = r.get(j);
+}
+template <int TH, bool SHORT>
+__device__ __forceinline__ void load8q(const int8_t* p, float scale, int t, int c, uint32_t cols, float* v) {
+    RawQ<TH, SHORT> r;
+    r.load(p, t, c, cols);
+    r.trim(t, c, cols);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = scale * r.get(j);
+}
+/* eight values to entries k .. of a row of n */
+template <class T>
+__device__ __forceinline__ void put8(T* row, uint32_t k, uint32_t n, const float* v) {
+    typename Vec<T>::v8 x;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = (T)v[j];
+    if (k + 8 <= n) __builtin_memcpy(row + k, &x, 16);
+    else
+#pragma unroll
+        for (int j = 0; j < 7; ++j)
+            if (k + j < n) row[k + j] = x[j];
+}
+template <class T, int TH>
+__device__ __forceinline__ void store8(T* p, int t, int c, uint32_t cols, const float* v) { put8<T>(p, row_col<TH>(t, c), cols, v); }
 
 /* ---- 8-bit checkpoints ------------------------------------------------------------------------------- */
 struct RowArgs {
@@ -252,7 +305,7 @@ __device__ __forceinline__ float finite_magnitude(float x) {
     const float a = fabsf(x);
     return a < INFINITY ? a : 0.0f;
 }
-template <class T, bool WIDE, int TH, int NCH>
+template <class T, int TH, int NCH, bool SHORT = false>
 __global__ __launch_bounds__(TH < 256 ? 256 : TH) void checkpoint_encode(const RowArgs a) {
     __shared__ float cells[2][16];
     const int t = threadIdx.x % TH;
@@ -262,7 +315,7 @@ __global__ __launch_bounds__(TH < 256 ? 256 : TH) void checkpoint_encode(const R
     for (uint64_t row = (uint64_t)blockIdx.x * SETS + threadIdx.x / TH; row < a.rows; row += (uint64_t)gridDim.x * SETS) {
         const T* src = (const T*)a.src + row * a.ld_src;
         int8_t* dst = (int8_t*)a.dst + row * a.ld_dst;
-        Raw<T, TH, WIDE> x[NCH ? NCH : 1];
+        Raw<T, TH, SHORT> x[NCH ? NCH : 1];
         /* magnitudes compare like their bits, two at a time */
         typedef uint16_t s2 __attribute__((ext_vector_type(2)));
         s2 top = {0, 0};
@@ -270,6 +323,7 @@ __global__ __launch_bounds__(TH < 256 ? 256 : TH) void checkpoint_encode(const R
         for (int c = 0; c < (NCH ? NCH : 1); ++c) x[c].load(src, t, c, a.cols);
         for (int c = 0; c < chunks; ++c) {
             if (!NCH) x[0].load(src, t, c, a.cols);
+            x[NCH ? c : 0].trim(t, c, a.cols);
 #pragma unroll
             for (int i = 0; i < 4; ++i) top = __builtin_elementwise_max(top, __builtin_bit_cast(s2, x[NCH ? c : 0].w[i] & 0x7FFF7FFFu));
         }
@@ -281,7 +335,10 @@ __global__ __launch_bounds__(TH < 256 ? 256 : TH) void checkpoint_encode(const R
         if (!numbers) {
             m = 0.0f;
             for (int c = 0; c < chunks; ++c) {
-                if (!NCH) x[0].load(src, t, c, a.cols);
+                if (!NCH) {
+                    x[0].load(src, t, c, a.cols);
+                    x[0].trim(t, c, a.cols);
+                }
 #pragma unroll
                 for (int j = 0; j < 8; ++j) m = fmaxf(m, finite_magnitude(x[NCH ? c : 0].get(j)));
             }
@@ -293,8 +350,11 @@ __global__ __launch_bounds__(TH < 256 ? 256 : TH) void checkpoint_encode(const R
         const bool plain = numbers && e > -100 && e < 100;
         const float times127 = plain ? ldexpf(127.0f, e) : 0.0f, quick = times127 * inv;
         for (int c = 0; c < chunks; ++c) {
-            if (!NCH) x[0].load(src, t, c, a.cols);
-            const Raw<T, TH, WIDE>& r = x[NCH ? c : 0];
+            if (!NCH) {
+                x[0].load(src, t, c, a.cols);
+                x[0].trim(t, c, a.cols);
+            }
+            const Raw<T, TH, SHORT>& r = x[NCH ? c : 0];
             uint32_t q[8];
             if (plain) {
 #pragma unroll
@@ -305,29 +365,28 @@ __global__ __launch_bounds__(TH < 256 ? 256 : TH) void checkpoint_encode(const R
             } else {
                 for (int j = 0; j < 8; ++j) q[j] = (uint32_t)(int)quantised(r.get(j), amax, inv, e);
             }
-            if (WIDE) {
-                const uint32_t k = row_col<TH, true>(t, c, 0);
+            {
+                const uint32_t k = row_col<TH>(t, c);
                 uint2 w;
                 w.x = __builtin_amdgcn_perm(__builtin_amdgcn_perm(q[3], q[2], 0x0C0C0400u), __builtin_amdgcn_perm(q[1], q[0], 0x0C0C0400u), 0x05040100u);
                 w.y = __builtin_amdgcn_perm(__builtin_amdgcn_perm(q[7], q[6], 0x0C0C0400u), __builtin_amdgcn_perm(q[5], q[4], 0x0C0C0400u), 0x05040100u);
-                if (k < a.cols) *(uint2*)(dst + k) = w;
-            } else {
-                for (int j = 0; j < 8; ++j) {
-                    const uint32_t k = row_col<TH, false>(t, c, j);
-                    if (k < a.cols) dst[k] = (int8_t)q[j];
-                }
+                if (k + 8 <= a.cols) __builtin_memcpy(dst + k, &w, 8);
+                else
+#pragma unroll
+                    for (int j = 0; j < 7; ++j)
+                        if (k + j < a.cols) dst[k + j] = (int8_t)q[j];
             }
         }
         if (TH > 64) __syncthreads();                    /* the cells are free again */
     }
 }
 /* 256 lanes take 2048 entries of a row */
-template <class T, bool WIDE>
+template <class T, bool SHORT>
 __global__ __launch_bounds__(256) void checkpoint_decode(const RowArgs a) {
     for (uint64_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
         float v[8];
-        load8q<256, WIDE>((const int8_t*)a.src + row * a.ld_src, a.scale[row], threadIdx.x, blockIdx.x, a.cols, v);
-        store8<T, 256, WIDE>((T*)a.dst + row * a.ld_dst, threadIdx.x, blockIdx.x, a.cols, v);
+        load8q<256, SHORT>((const int8_t*)a.src + row * a.ld_src, a.scale[row], threadIdx.x, blockIdx.x, a.cols, v);
+        store8<T, 256>((T*)a.dst + row * a.ld_dst, threadIdx.x, blockIdx.x, a.cols, v);
     }
 }
 
@@ -344,24 +403,42 @@ struct NormArgs {
     float eps;
     int centred;
 };
-template <class T, bool WIDE, int TH, int NCH>
+template <class T, int TH, int NCH, bool SHORT = false>
 __global__ __launch_bounds__(TH < 256 ? 256 : TH) void norm_forward(const NormArgs a) {
     __shared__ float cells[2][16];
     const int t = threadIdx.x % TH;
     constexpr uint32_t SETS = TH < 256 ? 256 / TH : 1;
     const float per = 1.0f / (float)a.cols;
-    Raw<T, TH, WIDE> g[NCH], b[NCH];                 /* under way while the sums are formed */
+    Raw<T, TH, SHORT> g[NCH], b[NCH];                 /* under way while the sums are formed */
 #pragma unroll
     for (int c = 0; c < NCH; ++c) {
         if (a.gamma) g[c].load((const T*)a.gamma, t, c, a.cols);
         if (a.beta) b[c].load((const T*)a.beta, t, c, a.cols);
     }
+    bool trimmed = false;
     for (uint64_t row = (uint64_t)blockIdx.x * SETS + threadIdx.x / TH; row < a.rows; row += (uint64_t)gridDim.x * SETS) {
         float x[NCH][8];
+        if (a.scale) {
+            const float scale = a.scale[row];
+            RawQ<TH, SHORT> r[NCH];
 #pragma unroll
-        for (int c = 0; c < NCH; ++c) {
-            if (a.scale) load8q<TH, WIDE>((const int8_t*)a.x + row * a.ldx, a.scale[row], t, c, a.cols, x[c]);
-            else load8<T, TH, WIDE>((const T*)a.x + row * a.ldx, t, c, a.cols, x[c]);
+            for (int c = 0; c < NCH; ++c) r[c].load((const int8_t*)a.x + row * a.ldx, t, c, a.cols);
+#pragma unroll
+            for (int c = 0; c < NCH; ++c) {
+                r[c].trim(t, c, a.cols);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[c][j] = scale * r[c].get(j);
+            }
+        } else {
+            Raw<T, TH, SHORT> r[NCH];
+#pragma unroll
+            for (int c = 0; c < NCH; ++c) r[c].load((const T*)a.x + row * a.ldx, t, c, a.cols);
+#pragma unroll
+            for (int c = 0; c < NCH; ++c) {
+                r[c].trim(t, c, a.cols);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[c][j] = r[c].get(j);
+            }
         }
         float mean = 0.0f;
         if (a.centred) {
@@ -377,11 +454,18 @@ __global__ __launch_bounds__(TH < 256 ? 256 : TH) void norm_forward(const NormAr
         for (int c = 0; c < NCH; ++c)
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float d = row_col<TH, WIDE>(t, c, j) < a.cols ? x[c][j] - mean : 0.0f;
+                const float d = row_col<TH>(t, c) + j < a.cols ? x[c][j] - mean : 0.0f;
                 x[c][j] = d;
                 s += d * d;
             }
         const float rstd = 1.0f / sqrtf(group_sum<TH>(s, cells[1], t) * per + a.eps);
+        if (!trimmed)
+#pragma unroll
+            for (int c = 0; c < NCH; ++c) {
+                if (a.gamma) g[c].trim(t, c, a.cols);
+                if (a.beta) b[c].trim(t, c, a.cols);
+            }
+        trimmed = true;
         if (t == 0) {
             if (a.mean) a.mean[row] = mean;
             if (a.rstd) a.rstd[row] = rstd;
@@ -395,7 +479,7 @@ __global__ __launch_bounds__(TH < 256 ? 256 : TH) void norm_forward(const NormAr
                 if (a.beta) v += b[c].get(j);
                 x[c][j] = v;
             }
-            store8<T, TH, WIDE>((T*)a.y + row * a.ldy, t, c, a.cols, x[c]);
+            store8<T, TH>((T*)a.y + row * a.ldy, t, c, a.cols, x[c]);
         }
         if (TH > 64) __syncthreads();                /* the cells are free again */
     }
@@ -416,7 +500,7 @@ struct NormBackArgs {
     uint32_t rows, cols;
     int centred;
 };
-template <class T, bool EIGHT, bool WIDE, int TH, int NCH, int LANES>
+template <class T, bool EIGHT, int TH, int NCH, int LANES, bool SHORT = false>
 __global__ __launch_bounds__(LANES) void norm_backward(const NormBackArgs a) {
     extern __shared__ float lds[];
     constexpr int SETS = LANES / TH;
@@ -427,19 +511,22 @@ __global__ __launch_bounds__(LANES) void norm_backward(const NormBackArgs a) {
     for (int c = 0; c < NCH; ++c)
 #pragma unroll
         for (int j = 0; j < 8; ++j) dg[c][j] = db[c][j] = 0.0f;
-    Raw<T, TH, WIDE> gamma[NCH];
+    Raw<T, TH, SHORT> gamma[NCH];
     if (a.gamma)
 #pragma unroll
-        for (int c = 0; c < NCH; ++c) gamma[c].load((const T*)a.gamma, t, c, a.cols);
+        for (int c = 0; c < NCH; ++c) {
+            gamma[c].load((const T*)a.gamma, t, c, a.cols);
+            gamma[c].trim(t, c, a.cols);
+        }
     const float per = 1.0f / (float)a.cols;
     const uint64_t step = (uint64_t)gridDim.x * SETS;
     /* A row is kept as it was read and unpacked twice, for the sums and for dx: two rows' raw bits take fewer registers than one row's values.
      * Where a lane has more than one chunk of a row there is no room for the next one. */
     constexpr bool AHEAD = NCH == 1;
-    typedef typename std::conditional<EIGHT, RawQ<TH, WIDE>, Raw<T, TH, WIDE>>::type RawX;
+    typedef typename std::conditional<EIGHT, RawQ<TH, SHORT>, Raw<T, TH, SHORT>>::type RawX;
     struct Row {
         RawX x[NCH];
-        Raw<T, TH, WIDE> dy[NCH];
+        Raw<T, TH, SHORT> dy[NCH];
         float mean, rstd, scale;
     };
     auto fetch = [&](Row& to, uint64_t row) {
@@ -460,10 +547,12 @@ __global__ __launch_bounds__(LANES) void norm_backward(const NormBackArgs a) {
         const uint32_t cols = row < a.rows ? a.cols : 0;
         float sg = 0.0f, sgx = 0.0f;
 #pragma unroll
-        for (int c = 0; c < NCH; ++c)
+        for (int c = 0; c < NCH; ++c) {
+            now.x[c].trim(t, c, cols);
+            now.dy[c].trim(t, c, cols);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const bool in = WIDE ? row_col<TH, true>(t, c, 0) < cols : row_col<TH, false>(t, c, j) < cols;
+                const bool in = row_col<TH>(t, c) + j < cols;
                 const float h = in ? (now.x[c].get(j) * now.scale - now.mean) * now.rstd : 0.0f, d = now.dy[c].get(j);
                 dg[c][j] += d * h;
                 db[c][j] += d;
@@ -471,6 +560,7 @@ __global__ __launch_bounds__(LANES) void norm_backward(const NormBackArgs a) {
                 sg += g;
                 sgx += g * h;
             }
+        }
         if (!a.dx) return;
         group_sum2<TH>(sg, sgx, cell, t);
         const float mg = a.centred ? sg * per : 0.0f, mgx = sgx * per;
@@ -484,7 +574,7 @@ __global__ __launch_bounds__(LANES) void norm_backward(const NormBackArgs a) {
                 const float h = (now.x[c].get(j) * now.scale - now.mean) * now.rstd, d = now.dy[c].get(j), g = a.gamma ? d * gamma[c].get(j) : d;
                 v[j] = now.rstd * (g - mg - h * mgx);
             }
-            store8<T, TH, WIDE>((T*)a.dx + row * a.lddx, t, c, cols, v);
+            store8<T, TH>((T*)a.dx + row * a.lddx, t, c, cols, v);
         }
     };
     float2 *cell0 = cells[0] + set * (TH / 64), *cell1 = cells[1] + set * (TH / 64);
@@ -519,7 +609,7 @@ __global__ __launch_bounds__(LANES) void norm_backward(const NormBackArgs a) {
             for (int c = 0; c < NCH; ++c)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const uint32_t k = row_col<TH, WIDE>(t, c, j);
+                    const uint32_t k = row_col<TH>(t, c) + j;
                     if (k >= a.cols) continue;
                     float v = which ? db[c][j] : dg[c][j];
                     if (s) v += lds[k];
@@ -584,7 +674,6 @@ struct ProductArgs {
     float* part;                     /* [split][nq][ldp] unfinished sums, where r is split; null: the whole of r in one go */
     uint64_t ldp;
     uint32_t r_split;                /* r of one split */
-    int wide_out;                    /* every row of the epilogue's tensors can be accessed in pieces of eight */
 };
 template <class T> __device__ __forceinline__ f4 mfma(typename Vec<T>::v8 a, typename Vec<T>::v8 b, f4 c);
 template <> __device__ __forceinline__ f4 mfma<_Float16>(Vec<_Float16>::v8 a, Vec<_Float16>::v8 b, f4 c) {
@@ -595,7 +684,7 @@ template <> __device__ __forceinline__ f4 mfma<__bf16>(Vec<__bf16>::v8 a, Vec<__
 }
 
 /* A tile of an operand: SIDE of p (or q) by BK of r, 32 or 64 */
-template <class T, bool ALONG, bool EIGHT, int SIDE, int BK>
+template <class T, bool ALONG, int SIDE, int BK>
 struct Tile {
     typedef typename Vec<T>::v8 v8;
     typedef short s4 __attribute__((ext_vector_type(4)));
@@ -606,24 +695,6 @@ struct Tile {
     __device__ static __forceinline__ int place(int line, int piece) {
         if (ALONG) return line * BK + ((piece ^ turn(line)) << 3);
         return line * SIDE + ((((piece >> 1) ^ spread(line)) << 1 | (piece & 1)) << 3);
-    }
-    /* eight elements along memory: (line, col .. col + 7) of an operand of lines x cols; outside: zeros */
-    __device__ static __forceinline__ v8 fetch(const Operand& o, uint64_t line, uint64_t lines, uint64_t col, uint64_t cols) {
-        v8 v = {0, 0, 0, 0, 0, 0, 0, 0};
-        if (line >= lines) return v;
-        for (int j = 0; j < 8; ++j)
-            if (col + j < cols) v[j] = EIGHT ? (T)(float)((const int8_t*)o.d)[line * o.ld + col + j] : ((const T*)o.d)[line * o.ld + col + j];
-        return v;
-    }
-    /* elements n * 8 .. of the tile whose corner is (side0, r0), by lane t of TH */
-    template <int TH>
-    __device__ static __forceinline__ void fill(T* lds, const Operand& o, uint64_t side0, uint64_t sides, uint64_t r0, uint64_t nr, int t) {
-        constexpr int PIECES = ALONG ? BK / 8 : SIDE / 8;
-        for (int n = t; n < ELEMENTS / 8; n += TH) {
-            const int line = n / PIECES, piece = n % PIECES;
-            const v8 v = ALONG ? fetch(o, side0 + line, sides, r0 + piece * 8, nr) : fetch(o, r0 + line, nr, side0 + piece * 8, sides);
-            *(v8*)(lds + place(line, piece)) = v;
-        }
     }
     /* the matrix instruction's operand: sixteen of p from `side` on, r from 32 s on */
     __device__ static __forceinline__ v8 fragment(const T* lds, int side, int s, int lane) {
@@ -641,21 +712,6 @@ struct Tile {
     }
 };
 
-/* eight neighbouring entries of a row of out, from column p on; whole: they are all there and lie on 16 bytes */
-template <class T>
-__device__ __forceinline__ void put8(void* base, uint64_t ld, uint32_t q, uint32_t p, uint32_t np, bool whole, const float* v) {
-    T* at = (T*)base + q * ld + p;
-    if (whole) {
-        typename Vec<T>::v8 x;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = (T)v[i];
-        *(typename Vec<T>::v8*)at = x;
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (p + i < np) at[i] = (T)v[i];
-    }
-}
 /* The epilogue of eight entries of column p on.  What it needs for the columns is loaded once, by the constructor; what it needs for the entries,
  * the residual, by ask(), ahead of apply(). */
 template <class T, bool FORWARD>
@@ -681,10 +737,11 @@ struct Finish {
     __device__ __forceinline__ void ask(uint32_t q) {
         if (!FORWARD || !a.residual || q >= a.nq || p >= a.np) return;
         const T* at = (const T*)a.residual + q * a.ldres + p;
-        if (a.wide_out) res = *(const typename Vec<T>::v8*)at;
+        if (p + 8 <= a.np) res = unaligned<typename Vec<T>::v8>(at);
         else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) res[i] = p + i < a.np ? at[i] : (T)0.0f;
+            for (int i = 0; i < 7; ++i)
+                if (p + i < a.np) res[i] = at[i];
         }
     }
     __device__ __forceinline__ void apply(uint32_t q, float* v) const {
@@ -698,7 +755,7 @@ struct Finish {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[i] += bias[i];
             }
-            if (a.z) put8<T>(a.z, a.ldz, q, p, a.np, a.wide_out, v);
+            if (a.z) put8<T>((T*)a.z + q * a.ldz, p, a.np, v);
             if (a.act != TC_ACT_NONE) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[i] = activate(v[i], a.act);
@@ -711,7 +768,7 @@ struct Finish {
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] *= scale[0];
         }
-        put8<T>(a.out, a.ldo, q, p, a.np, a.wide_out, v);
+        put8<T>((T*)a.out + q * a.ldo, p, a.np, v);
     }
 };
 /* A wave's NP x NQ blocks of sixteen by sixteen, through a piece of LDS of its own (NP * 16 + 4 floats for each of sixteen q): a lane of
@@ -752,40 +809,11 @@ __device__ __forceinline__ void drain(const ProductArgs& a, f4 (&acc)[NP][NQ], u
     }
 }
 
-template <class T, bool P_ALONG, bool P_EIGHT, bool Q_ALONG, bool FORWARD>
-__global__ __launch_bounds__(256) void product(const ProductArgs a) {
-    constexpr int SP = 128, SQ = 128, BK = 64;
-    typedef Tile<T, P_ALONG, P_EIGHT, SP, BK> TP;
-    typedef Tile<T, Q_ALONG, false, SQ, BK> TQ;
-    __shared__ __align__(16) uint8_t lds[(TP::ELEMENTS + TQ::ELEMENTS) * sizeof(T)];
-    T *lp = (T*)lds, *lq = lp + TP::ELEMENTS;
-    const uint32_t tiles_p = (a.np + SP - 1) / SP;
-    const uint64_t p0 = (uint64_t)(blockIdx.x % tiles_p) * SP, q0 = (uint64_t)(blockIdx.x / tiles_p) * SQ;
-    const int t = threadIdx.x, lane = t & 63, wp = (t >> 6) & 1, wq = t >> 7;
-    f4 acc[4][4] = {};
-#pragma unroll 1
-    for (uint32_t r0 = 0; r0 < a.nr; r0 += BK) {
-        __syncthreads();
-        TP::template fill<256>(lp, a.p, p0, a.np, r0, a.nr, t);
-        TQ::template fill<256>(lq, a.q, q0, a.nq, r0, a.nr, t);
-        __syncthreads();
-        for (int s = 0; s < 2; ++s) {
-            typename Vec<T>::v8 fp[4], fq[4];
-            for (int i = 0; i < 4; ++i) fp[i] = TP::fragment(lp, wp * 64 + i * 16, s, lane);
-            for (int j = 0; j < 4; ++j) fq[j] = TQ::fragment(lq, wq * 64 + j * 16, s, lane);
-            for (int i = 0; i < 4; ++i)
-                for (int j = 0; j < 4; ++j) acc[i][j] = mfma<T>(fp[i], fq[j], acc[i][j]);
-        }
-    }
-    __syncthreads();
-    drain<T, FORWARD, 4, 4>(a, acc, lds + (t >> 6) * drain_bytes<4>(), (uint32_t)q0 + wq * 64, (uint32_t)p0 + wp * 64, 0, lane);
-}
-
-/* ---- products of aligned operands --------------------------------------------------------------------------
- * The same product where both operands can be read in 16-byte pieces (int8: 8-byte ones).  16-bit tiles go from memory to LDS without
+/* How a tile gets to LDS.  An operand whose rows can be read in aligned 16-byte pieces (int8: 8-byte ones) goes there directly, without
  * passing through registers.  That direct load writes the lanes' pieces side by side, so the places of a tile are dealt out
  * on the memory side: place n takes the piece that belongs there.  Buffer addresses: a piece outside the operand gets an offset past the buffer's end and reads
- * zeros.  int8 tiles pass through registers, where they become the other operand's type. */
+ * zeros.  int8 tiles pass through registers, where they become the other operand's type.  So do LOOSE operands, rows of any
+ * alignment, length and stride: pieces at addresses that need not be aligned (1), or entry by entry where a row has fewer than eight (2). */
 /* eight int8 in two words -> eight of T, exactly.  float16: a byte with its sign bit flipped is q + 128; put under the exponent of 1024 it reads 1152 + q. */
 template <class T> __device__ __forceinline__ typename Vec<T>::v8 widen(uint32_t lo, uint32_t hi);
 template <> __device__ __forceinline__ Vec<_Float16>::v8 widen<_Float16>(uint32_t lo, uint32_t hi) {
@@ -816,14 +844,17 @@ template <> __device__ __forceinline__ Vec<__bf16>::v8 widen<__bf16>(uint32_t lo
     }
     return u.v;
 }
-template <class T, bool ALONG, bool EIGHT, int SIDE, int TH, int BK>
+template <class T, bool ALONG, bool EIGHT, int LOOSE, int SIDE, int TH, int BK>
 struct Feed {
-    typedef Tile<T, ALONG, EIGHT, SIDE, BK> tile;
-    typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+    typedef Tile<T, ALONG, SIDE, BK> tile;
     static constexpr int N = SIDE * BK / 8 / TH, PIECES = ALONG ? BK / 8 : SIDE / 8, SIZE = EIGHT ? 1 : 2;
+    static constexpr bool HELD = EIGHT || LOOSE != 0, SHORT = LOOSE == 2;
     static constexpr uint32_t NOWHERE = 0x80000000u;
-    typedef u2 Held[EIGHT ? N : 1];
-    uint32_t off[N];
+    typedef uint32_t Held[HELD ? N : 1][EIGHT ? 2 : 4];
+    typename std::conditional<LOOSE != 0, uint64_t, uint32_t>::type off[N];
+    uint32_t have[LOOSE ? N : 1];    /* entries of a piece that the operand has, as far as the axis across the sum says */
+    uint32_t count[LOOSE ? N : 1];   /* entries of the pieces in `held` */
+    bool ragged;                     /* some of them are not whole (the same for all lanes) */
     const char* base;
     uint64_t step;
     uint32_t nr, line_bytes;
@@ -837,37 +868,67 @@ struct Feed {
         line_bytes = (uint32_t)(o.ld * SIZE);
         base = (const char*)o.d + (ALONG ? side0 * o.ld + r0 : r0 * o.ld + side0) * SIZE;
         step = ALONG ? BK * SIZE : BK * o.ld * SIZE;
+        ragged = !ALONG && sides - side0 < SIDE && sides % 8;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int n = i * TH + t, line = n / PIECES, piece = piece_of(n);
-            const bool in = side0 + (ALONG ? line : piece * 8) < sides;
-            off[i] = in ? line * line_bytes + piece * 8 * SIZE : NOWHERE;
+            const uint64_t side = side0 + (ALONG ? line : piece * 8);
+            if (LOOSE) {
+                off[i] = (line * o.ld + piece * 8) * SIZE;
+                have[i] = side >= sides ? 0 : ALONG || sides - side >= 8 ? 8 : (uint32_t)(sides - side);
+            } else off[i] = side < sides ? line * line_bytes + piece * 8 * SIZE : NOWHERE;
         }
     }
     /* tile number k, to its place in LDS or into `held`; past the last one: zeros */
     __device__ __forceinline__ void issue(T* lds, Held& held, uint32_t k, int t) {
         const uint32_t rest = __builtin_amdgcn_readfirstlane(nr > k * BK ? nr - k * BK : 0);      /* a saturating difference, which is a vector instruction */
         const char* at = base + (rest ? k * step : 0);
-        const uint32_t span = ALONG ? NOWHERE - 1 : (rest < BK ? rest : BK) * line_bytes;
-        const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)at, 0, span, 0x00020000);
-        if (ALONG && rest < BK) {        /* the last tile of r: pieces past its end go, for good */
-            asm volatile("");            /* a branch, not eight selections in every step */
+        if constexpr (LOOSE) {
+            typedef typename std::conditional<EIGHT, uint8_t, uint16_t>::type entry;
+            if (ALONG) ragged = rest < BK && rest % 8;
 #pragma unroll
-            for (int i = 0; i < N; ++i)
-                if ((uint32_t)piece_of(i * TH + t) * 8 >= rest) off[i] = NOWHERE;
-        }
+            for (int i = 0; i < N; ++i) {
+                const int n = i * TH + t;
+                const uint32_t r = ALONG ? piece_of(n) * 8 : n / PIECES, left = rest > r ? rest - r : 0;
+                count[i] = ALONG ? (left < have[i] ? left : have[i]) : (left ? have[i] : 0);
+                read_piece<SHORT>((const entry*)(at + off[i]), count[i], held[i]);
+            }
+        } else {
+            const uint32_t span = ALONG ? NOWHERE - 1 : (rest < BK ? rest : BK) * line_bytes;
+            const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)at, 0, span, 0x00020000);
+            if (ALONG && rest < BK) {    /* the last tile of r: pieces past its end go, for good */
+                asm volatile("");        /* a branch, not eight selections in every step */
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            uint32_t o = off[i];
-            if (EIGHT) held[i] = __builtin_amdgcn_raw_buffer_load_b64(r, o, 0, 0);
-            else
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(lds + (i * TH + (t & ~63)) * 8), 16, o, 0, 0, 0);
+                for (int i = 0; i < N; ++i)
+                    if ((uint32_t)piece_of(i * TH + t) * 8 >= rest) off[i] = NOWHERE;
+            }
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                uint32_t o = off[i];
+                if constexpr (EIGHT) {
+                    const auto x = __builtin_amdgcn_raw_buffer_load_b64(r, o, 0, 0);
+                    held[i][0] = x[0];
+                    held[i][1] = x[1];
+                } else
+                    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(lds + (i * TH + (t & ~63)) * 8), 16, o, 0, 0, 0);
+            }
         }
     }
     __device__ __forceinline__ void settle(T* lds, Held& held, int t) {
-        if (!EIGHT) return;
+        if constexpr (HELD) {
+            if (LOOSE == 1 && ragged) {
+                asm volatile("");        /* a branch */
 #pragma unroll
-        for (int i = 0; i < N; ++i) *(typename Vec<T>::v8*)(lds + (i * TH + t) * 8) = widen<T>(held[i][0], held[i][1]);
+                for (int i = 0; i < N; ++i)
+                    if (count[i] && count[i] < 8) to_front(held[i], count[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                typename Vec<T>::v8* to = (typename Vec<T>::v8*)(lds + (i * TH + t) * 8);
+                if constexpr (EIGHT) *to = widen<T>(held[i][0], held[i][1]);
+                else *to = __builtin_bit_cast(typename Vec<T>::v8, make_uint4(held[i][0], held[i][1], held[i][2], held[i][3]));
+            }
+        }
     }
 };
 /* Workgroups go to the eight XCDs in turn, each with an L2 of its own: an XCD takes neighbouring tiles, in blocks of four along q */
@@ -884,8 +945,8 @@ __device__ __forceinline__ void tile_of(uint32_t b, uint32_t tiles_p, uint32_t t
 /* What both kernels below start with: the tile of this workgroup and its part of r */
 #define TC_PRODUCT_PROLOGUE                                                                                                 \
     constexpr int TH = WP * WQ * 64, NP = SP / WP / 16, NQ = SQ / WQ / 16, STAGE = (SP + SQ) * BK;                          \
-    typedef Feed<T, P_ALONG, P_EIGHT, SP, TH, BK> FP;                                                                       \
-    typedef Feed<T, Q_ALONG, false, SQ, TH, BK> FQ;                                                                         \
+    typedef Feed<T, P_ALONG, P_EIGHT, LOOSE, SP, TH, BK> FP;                                                                \
+    typedef Feed<T, Q_ALONG, false, LOOSE, SQ, TH, BK> FQ;                                                                  \
     extern __shared__ __align__(16) uint8_t lds_bytes[];                                                                    \
     T* const lds = (T*)lds_bytes;                                                                                           \
     const uint32_t tiles_p = (a.np + SP - 1) / SP, tiles_q = (a.nq + SQ - 1) / SQ;                                          \
@@ -906,7 +967,7 @@ __device__ __forceinline__ void tile_of(uint32_t b, uint32_t tiles_p, uint32_t t
     drain<T, FORWARD, NP, NQ>(a, acc, lds_bytes + w * drain_bytes<NP>(), (uint32_t)q0 + wq * (SQ / WQ), (uint32_t)p0 + wp * (SP / WP), split, lane);
 
 /* Two stages of 64 r: one is multiplied while the other is filled; the two or more workgroups that share a compute unit cover each other's waits. */
-template <class T, bool P_ALONG, bool P_EIGHT, bool Q_ALONG, bool FORWARD, int SP, int SQ, int WP, int WQ>
+template <class T, bool P_ALONG, bool P_EIGHT, bool Q_ALONG, bool FORWARD, int LOOSE, int SP, int SQ, int WP, int WQ>
 __global__ __launch_bounds__(WP * WQ * 64) void product_paired(const ProductArgs a) {
     constexpr int BK = 64;
     TC_PRODUCT_PROLOGUE
@@ -915,6 +976,7 @@ __global__ __launch_bounds__(WP * WQ * 64) void product_paired(const ProductArgs
     fp.issue(lds, hp, 0, t);
     fq.issue(lds + SP * BK, hq, 0, t);
     fp.settle(lds, hp, t);
+    fq.settle(lds + SP * BK, hq, t);
 #pragma unroll 1
     for (uint32_t k = 0; k < steps; ++k) {
         T* now = lds + (k & 1) * STAGE;
@@ -935,6 +997,7 @@ __global__ __launch_bounds__(WP * WQ * 64) void product_paired(const ProductArgs
                 for (int j = 0; j < NQ; ++j) acc[i][j] = mfma<T>(x[i], y[j], acc[i][j]);
         }
         fp.settle(next, hp, t);
+        fq.settle(next + SP * BK, hq, t);
     }
     TC_PRODUCT_EPILOGUE
 }
@@ -948,6 +1011,7 @@ template <class T, bool P_ALONG, bool Q_ALONG, bool FORWARD, int SP, int SQ, int
 __global__ __launch_bounds__(WP * WQ * 64) __attribute__((amdgpu_waves_per_eu(WP * WQ / 4, WP * WQ / 4))) void product_deep(const ProductArgs a) {
     constexpr int BK = 32, STAGES = 5;
     constexpr bool P_EIGHT = false;
+    constexpr int LOOSE = 0;
     TC_PRODUCT_PROLOGUE
     constexpr int LOADS = FP::N + FQ::N;
     typename FP::Held hp;
@@ -1029,62 +1093,85 @@ __global__ __launch_bounds__(256) void join_parts(const ProductArgs a, uint32_t 
 /* ---- a few rows -------------------------------------------------------------------------------------------------
  * y = x w^T for at most sixteen rows of x: the weights are read once and that is all it costs.  A workgroup has sixteen of w's rows and its waves share r; each goes from memory
  * straight into the matrix instruction: lane l takes 16 r of row l & 15, from 16 (l >> 4) on, the first eight of them for one
- * instruction and the last eight for the next (any order of r does, if both operands have the same).  The waves' sums are added in order. */
-template <class T, bool EIGHT, int WAVES>
+ * instruction and the last eight for the next (any order of r does, if both operands have the same).  The waves' sums are added in order.
+ * A wave has AHEAD chunks of 64 r under way.  LOOSE: rows of any alignment and of any length from eight on. */
+template <class T, bool EIGHT, bool LOOSE, int WAVES>
 __global__ __launch_bounds__(WAVES * 64) void product_thin(const ProductArgs a) {
     typedef typename Vec<T>::v8 v8;
-    typedef uint32_t u4 __attribute__((ext_vector_type(4)));
     __shared__ float sums[WAVES][256];
     const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6);
-    const uint32_t p0 = blockIdx.x * 16, line = lane & 15;
-    constexpr int SIZE = EIGHT ? 1 : 2;
+    const uint32_t p0 = blockIdx.x * 16, line = lane & 15, at = (lane >> 4) * 16;
+    constexpr int SIZE = EIGHT ? 1 : 2, WORDS = EIGHT ? 2 : 4;
     constexpr uint32_t NOWHERE = 0x80000000u;
-    const __amdgpu_buffer_rsrc_t rp = __builtin_amdgcn_make_buffer_rsrc((char*)a.p.d + p0 * a.p.ld * SIZE, 0, NOWHERE - 1, 0x00020000);
-    const __amdgpu_buffer_rsrc_t rq = __builtin_amdgcn_make_buffer_rsrc((void*)a.q.d, 0, NOWHERE - 1, 0x00020000);
-    const uint32_t at = (lane >> 4) * 16;
-    const uint32_t op = p0 + line < a.np ? (uint32_t)(line * a.p.ld + at) * SIZE : NOWHERE, oq = line < a.nq ? (uint32_t)(line * a.q.ld + at) * 2 : NOWHERE;
+    const bool has_p = p0 + line < a.np, has_q = line < a.nq;
     f4 acc = {0, 0, 0, 0};
     constexpr int AHEAD = EIGHT ? 8 : 4;
     const uint32_t chunks = (a.nr + 63) / 64;
     for (uint32_t c = w; c < chunks; c += WAVES * AHEAD) {
-        u4 x[AHEAD][EIGHT ? 1 : 2];
-        auto place = [&](int i, uint32_t off, uint32_t& from) {
-            const uint32_t r = (c + i * WAVES) * 64;
-            from = r < a.nr ? r : 0;
-            return r + at < a.nr ? off : NOWHERE;
-        };
+        uint32_t x[AHEAD][2][WORDS], y[AHEAD][2][4];
+        if constexpr (LOOSE) {
+            const char* rp = (const char*)a.p.d + (has_p ? p0 + line : p0) * a.p.ld * SIZE;
+            const char* rq = (const char*)a.q.d + (has_q ? line : 0) * a.q.ld * 2;
+            typedef typename std::conditional<EIGHT, uint8_t, uint16_t>::type entry;
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i) {
-            uint32_t from;
-            const uint32_t o = place(i, op, from);
-            x[i][0] = __builtin_amdgcn_raw_buffer_load_b128(rp, o, from * SIZE, 0);
-            if constexpr (!EIGHT) x[i][1] = __builtin_amdgcn_raw_buffer_load_b128(rp, o == NOWHERE ? NOWHERE : o + 16, from * SIZE, 0);
-        }
-        /* the rows of x come from the caches, two chunks at a time */
+            for (int i = 0; i < AHEAD; ++i)
 #pragma unroll
-        for (int i = 0; i < AHEAD; i += 2) {
-            u4 y[2][2];
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                uint32_t from;
-                const uint32_t o = place(i + k, oq, from);
-                y[k][0] = __builtin_amdgcn_raw_buffer_load_b128(rq, o, from * 2, 0);
-                y[k][1] = __builtin_amdgcn_raw_buffer_load_b128(rq, o == NOWHERE ? NOWHERE : o + 16, from * 2, 0);
-            }
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                v8 lo, hi;
-                if constexpr (EIGHT) {
-                    lo = widen<T>(x[i + k][0][0], x[i + k][0][1]);
-                    hi = widen<T>(x[i + k][0][2], x[i + k][0][3]);
-                } else {
-                    lo = __builtin_bit_cast(v8, x[i + k][0]);
-                    hi = __builtin_bit_cast(v8, x[i + k][1]);
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t r = (c + i * WAVES) * 64 + at + h * 8, n = entries_at(r, a.nr);
+                    read_piece<false>((const entry*)rp + r, has_p ? n : 0, x[i][h]);
+                    read_piece<false>((const uint16_t*)rq + r, has_q ? n : 0, y[i][h]);
                 }
-                acc = mfma<T>(lo, __builtin_bit_cast(v8, y[k][0]), acc);
-                acc = mfma<T>(hi, __builtin_bit_cast(v8, y[k][1]), acc);
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i)
+                if ((c + i * WAVES) * 64 + 64 > a.nr)          /* the last chunk */
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const uint32_t n = entries_at((c + i * WAVES) * 64 + at + h * 8, a.nr);
+                        if (n && n < 8) {
+                            to_front(x[i][h], n);
+                            to_front(y[i][h], n);
+                        }
+                    }
+        } else {
+            const __amdgpu_buffer_rsrc_t rp = __builtin_amdgcn_make_buffer_rsrc((char*)a.p.d + p0 * a.p.ld * SIZE, 0, NOWHERE - 1, 0x00020000);
+            const __amdgpu_buffer_rsrc_t rq = __builtin_amdgcn_make_buffer_rsrc((void*)a.q.d, 0, NOWHERE - 1, 0x00020000);
+            const uint32_t op = (uint32_t)(line * a.p.ld + at) * SIZE, oq = (uint32_t)(line * a.q.ld + at) * 2;
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) {
+                const uint32_t r = (c + i * WAVES) * 64, from = r < a.nr ? r : 0;
+                const bool in = r + at < a.nr;                 /* the rows are whole pieces of sixteen */
+                const auto one = __builtin_amdgcn_raw_buffer_load_b128(rp, in && has_p ? op : NOWHERE, from * SIZE, 0);
+                if constexpr (EIGHT) {
+                    x[i][0][0] = one[0];
+                    x[i][0][1] = one[1];
+                    x[i][1][0] = one[2];
+                    x[i][1][1] = one[3];
+                } else {
+                    const auto two = __builtin_amdgcn_raw_buffer_load_b128(rp, in && has_p ? op + 16 : NOWHERE, from * SIZE, 0);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        x[i][0][k] = one[k];
+                        x[i][1][k] = two[k];
+                    }
+                }
+                const auto lo = __builtin_amdgcn_raw_buffer_load_b128(rq, in && has_q ? oq : NOWHERE, from * 2, 0);
+                const auto hi = __builtin_amdgcn_raw_buffer_load_b128(rq, in && has_q ? oq + 16 : NOWHERE, from * 2, 0);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    y[i][0][k] = lo[k];
+                    y[i][1][k] = hi[k];
+                }
             }
         }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                v8 u;
+                if constexpr (EIGHT) u = widen<T>(x[i][h][0], x[i][h][1]);
+                else u = __builtin_bit_cast(v8, make_uint4(x[i][h][0], x[i][h][1], x[i][h][2], x[i][h][3]));
+                acc = mfma<T>(u, __builtin_bit_cast(v8, make_uint4(y[i][h][0], y[i][h][1], y[i][h][2], y[i][h][3])), acc);
+            }
     }
     /* acc: q = lane & 15, p from 4 (lane >> 4) on */
 #pragma unroll
@@ -1136,44 +1223,47 @@ __global__ __launch_bounds__(1024) void scale_peak(const float* x, uint32_t nx, 
     m[2 * blockIdx.x + 1] = ldexpf(1.0f, -e);
 }
 /* A wave takes 512 columns (eight to a lane), the four waves of a workgroup every fourth of its rows. */
-template <class T, bool WIDE>
+template <class T, bool SHORT>
 __global__ __launch_bounds__(256) void slopes(const SlopeArgs a) {
     __shared__ float cells[4][512];
-    const int w = threadIdx.x >> 6, t = threadIdx.x & 63;
-    const uint32_t c0 = blockIdx.x * 512;
-    const uint32_t cols = a.cols - c0 < 512 ? a.cols - c0 : 512;
+    const int w = threadIdx.x >> 6, t = threadIdx.x & 63, strip = blockIdx.x;
+    const uint32_t k = row_col<64>(t, strip);
     float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0}, ws[8];
     const float mx = a.by_x && a.m ? a.m[1] : 1.0f, mw = a.by_w && a.m ? a.m[3] : 1.0f;
     if (a.by_w)
-        for (int j = 0; j < 8; ++j) {
-            const uint32_t k = row_col<64, WIDE>(t, 0, j);
-            ws[j] = k < cols ? a.w_scale[c0 + k] * mw : 0.0f;
-        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) ws[j] = k + j < a.cols ? a.w_scale[k + j] * mw : 0.0f;
     for (uint64_t row = (uint64_t)blockIdx.y * 4 + w; row < a.rows; row += (uint64_t)gridDim.y * 4) {
         float v[8], z[8];
-        load8<T, 64, WIDE>((const T*)a.dy + row * a.lddy + c0, t, 0, cols, v);
+        load8<T, 64, SHORT>((const T*)a.dy + row * a.lddy, t, strip, a.cols, v);
         if (a.act != TC_ACT_NONE) {
-            if (a.z_scale) load8q<64, WIDE>((const int8_t*)a.z + row * a.ldz + c0, a.z_scale[row], t, 0, cols, z);
-            else load8<T, 64, WIDE>((const T*)a.z + row * a.ldz + c0, t, 0, cols, z);
+            if (a.z_scale) load8q<64, SHORT>((const int8_t*)a.z + row * a.ldz, a.z_scale[row], t, strip, a.cols, z);
+            else load8<T, 64, SHORT>((const T*)a.z + row * a.ldz, t, strip, a.cols, z);
+#pragma unroll
             for (int j = 0; j < 8; ++j) v[j] *= slope(z[j], a.act);
-            if (a.dz) store8<T, 64, WIDE>((T*)a.dz + row * a.lddz + c0, t, 0, cols, v);
+            put8<T>((T*)a.dz + row * a.lddz, k, a.cols, v);
         }
+#pragma unroll
         for (int j = 0; j < 8; ++j) sum[j] += v[j];
         if (a.by_x) {
             const float f = a.x_scale[row] * mx;
+#pragma unroll
             for (int j = 0; j < 8; ++j) z[j] = v[j] * f;
-            store8<T, 64, WIDE>((T*)a.by_x + row * a.ld_by + c0, t, 0, cols, z);
+            put8<T>((T*)a.by_x + row * a.ld_by, k, a.cols, z);
         }
         if (a.by_w) {
+#pragma unroll
             for (int j = 0; j < 8; ++j) z[j] = v[j] * ws[j];
-            store8<T, 64, WIDE>((T*)a.by_w + row * a.ld_by + c0, t, 0, cols, z);
+            put8<T>((T*)a.by_w + row * a.ld_by, k, a.cols, z);
         }
     }
     if (!a.part) return;
-    for (int j = 0; j < 8; ++j) cells[w][row_col<64, WIDE>(t, 0, j)] = sum[j];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) cells[w][t * 8 + j] = sum[j];
     __syncthreads();
-    for (uint32_t k = threadIdx.x; k < cols; k += 256)
-        a.part[(uint64_t)blockIdx.y * a.cols + c0 + k] = (cells[0][k] + cells[1][k]) + (cells[2][k] + cells[3][k]);
+    const uint32_t first = strip * 512;
+    for (uint32_t i = threadIdx.x; i < 512 && first + i < a.cols; i += 256)
+        a.part[(uint64_t)blockIdx.y * a.cols + first + i] = (cells[0][i] + cells[1][i]) + (cells[2][i] + cells[3][i]);
 }
 template <class T>
 __global__ __launch_bounds__(256) void fill_rows(T* out, uint64_t ld, uint32_t rows, uint32_t cols) {

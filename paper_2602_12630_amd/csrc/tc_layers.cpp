@@ -81,12 +81,12 @@ uint32_t slope_groups(uint32_t rows, uint32_t cols) {
 /* How a product of np x nq results over nr is laid out: the tile, and into how many parts r is split so that there are workgroups for
  * the whole chip. */
 struct ProductPlan {
-    uint32_t np, nq, side_p, side_q, splits, r_split;
+    uint32_t np, nq, side, splits, r_split;
     uint64_t ldp;
     uint64_t tiles(uint32_t sp, uint32_t sq) const { return (uint64_t)((np + sp - 1) / sp) * ((nq + sq - 1) / sq); }
     size_t part_bytes() const { return splits > 1 ? (size_t)splits * nq * ldp * 4 : 0; }
     /* with the 16-bit copy of an int8 operand, which the kernel of the largest tiles wants */
-    size_t bytes(uint32_t nr) const { return part_bytes() + (side_p == 256 ? up((size_t)np * nr * 2, 256) : 0); }
+    size_t bytes(uint32_t nr) const { return part_bytes() + (side == 256 ? up((size_t)np * nr * 2, 256) : 0); }
 };
 /* Chosen by what the layouts cost, in microseconds, measured over products of 10^9 to 10^12 multiply-adds: so much for a step of 64 r
  * with one, two .. workgroups on every compute unit (as many as LDS holds), one for a round of workgroups to start and finish in, and
@@ -100,12 +100,12 @@ ProductPlan product_plan(uint32_t np, uint32_t nq, uint32_t nr) {
     };
     static const Layout layouts[3] = {{256, 1, {1.7}}, {128, 2, {0.75, 0.97}}, {64, 5, {0.48, 0.5, 0.62, 0.75, 0.9}}};
     static const uint32_t parts[] = {1, 2, 3, 4, 6, 8, 12, 16};
-    ProductPlan best = {np, nq, 64, 64, 1, nr, up(np, 8)};
+    ProductPlan best = {np, nq, 64, 1, nr, up(np, 8)};
     if (!nq || !nr) return best;                     /* no rows: nothing is launched */
     double least = 1e300;
     for (const Layout& l : layouts)
         for (uint32_t splits : parts) {
-            ProductPlan p = {np, nq, l.side, l.side, 1, nr, up(np, 8)};
+            ProductPlan p = {np, nq, l.side, 1, nr, up(np, 8)};
             if (splits > 1) {
                 p.r_split = (uint32_t)up((nr + splits - 1) / splits, 64);
                 p.splits = (nr + p.r_split - 1) / p.r_split;
@@ -155,55 +155,52 @@ using namespace tc::layers;
         if (e_) return ctx_fail_hip(ctx, e_, "launch of " #kernel);                         \
     } while (0)
 
-/* sixteen-byte accesses to 16-bit rows, eight-byte ones to int8 rows */
-bool wide(const void* p, uint64_t ld, uint32_t rows, uint32_t cols, int dtype) {
-    const uintptr_t mask = dtype == TC_I8 ? 7u : 15u;
-    return ((uintptr_t)p & mask) == 0 && cols % 8 == 0 && (rows <= 1 || ld % 8 == 0);
-}
-bool wide(const tc_matrix* m) { return wide(m->d_data, m->ld, m->rows, m->cols, m->dtype); }
-
 /* workgroups for `sets` sets of rows; the kernels go round until all are done */
 uint32_t row_grid(uint64_t sets) { return (uint32_t)std::min<uint64_t>(sets, 1u << 20); }
-template <class T, bool WIDE>
+template <class T>
 int encode_rows(tc_ctx* ctx, const RowArgs& a) {
     const uint32_t c = a.cols;
-    if (c <= 512) LAUNCH((checkpoint_encode<T, WIDE, 64, 1>), row_grid(((uint64_t)a.rows + 3) / 4), 256, 0, a);
-    else if (c <= 2048) LAUNCH((checkpoint_encode<T, WIDE, 256, 1>), row_grid(a.rows), 256, 0, a);
-    else if (c <= 4096) LAUNCH((checkpoint_encode<T, WIDE, 256, 2>), row_grid(a.rows), 256, 0, a);
-    else if (c <= 8192) LAUNCH((checkpoint_encode<T, WIDE, 256, 4>), row_grid(a.rows), 256, 0, a);
-    else if (c <= 16384) LAUNCH((checkpoint_encode<T, WIDE, 256, 8>), row_grid(a.rows), 256, 0, a);
-    else LAUNCH((checkpoint_encode<T, WIDE, 1024, 0>), row_grid(a.rows), 1024, 0, a);
+    if (c < 8) LAUNCH((checkpoint_encode<T, 64, 1, true>), row_grid(((uint64_t)a.rows + 3) / 4), 256, 0, a);
+    else if (c <= 512) LAUNCH((checkpoint_encode<T, 64, 1>), row_grid(((uint64_t)a.rows + 3) / 4), 256, 0, a);
+    else if (c <= 2048) LAUNCH((checkpoint_encode<T, 256, 1>), row_grid(a.rows), 256, 0, a);
+    else if (c <= 4096) LAUNCH((checkpoint_encode<T, 256, 2>), row_grid(a.rows), 256, 0, a);
+    else if (c <= 8192) LAUNCH((checkpoint_encode<T, 256, 4>), row_grid(a.rows), 256, 0, a);
+    else if (c <= 16384) LAUNCH((checkpoint_encode<T, 256, 8>), row_grid(a.rows), 256, 0, a);
+    else LAUNCH((checkpoint_encode<T, 1024, 0>), row_grid(a.rows), 1024, 0, a);
     return TC_OK;
 }
-template <class T, bool WIDE>
+template <class T>
 int norm_rows(tc_ctx* ctx, const NormArgs& a) {
     const uint32_t c = a.cols;
-    if (c <= 512) LAUNCH((norm_forward<T, WIDE, 64, 1>), row_grid(((uint64_t)a.rows + 3) / 4), 256, 0, a);
-    else if (c <= 2048) LAUNCH((norm_forward<T, WIDE, 256, 1>), row_grid(a.rows), 256, 0, a);
-    else if (c <= 4096) LAUNCH((norm_forward<T, WIDE, 256, 2>), row_grid(a.rows), 256, 0, a);
-    else if (c <= 8192) LAUNCH((norm_forward<T, WIDE, 256, 4>), row_grid(a.rows), 256, 0, a);
-    else if (c <= 16384) LAUNCH((norm_forward<T, WIDE, 1024, 2>), row_grid(a.rows), 1024, 0, a);
-    else LAUNCH((norm_forward<T, WIDE, 1024, 4>), row_grid(a.rows), 1024, 0, a);
+    if (c < 8) LAUNCH((norm_forward<T, 64, 1, true>), row_grid(((uint64_t)a.rows + 3) / 4), 256, 0, a);
+    else if (c <= 512) LAUNCH((norm_forward<T, 64, 1>), row_grid(((uint64_t)a.rows + 3) / 4), 256, 0, a);
+    else if (c <= 2048) LAUNCH((norm_forward<T, 256, 1>), row_grid(a.rows), 256, 0, a);
+    else if (c <= 4096) LAUNCH((norm_forward<T, 256, 2>), row_grid(a.rows), 256, 0, a);
+    else if (c <= 8192) LAUNCH((norm_forward<T, 256, 4>), row_grid(a.rows), 256, 0, a);
+    else if (c <= 16384) LAUNCH((norm_forward<T, 1024, 2>), row_grid(a.rows), 1024, 0, a);
+    else LAUNCH((norm_forward<T, 1024, 4>), row_grid(a.rows), 1024, 0, a);
     return TC_OK;
 }
-template <class T, bool EIGHT, bool WIDE>
+template <class T, bool EIGHT>
 int norm_back_rows(tc_ctx* ctx, const NormBackArgs& a, uint32_t groups) {
     const uint32_t c = a.cols, sets = norm_back_sets(a.rows, c);
     const size_t lds = sets > 1 ? (size_t)c * 4 : 0;
     if (a.rows < 1024) {                             /* few rows: smaller workgroups, so that they go to more compute units */
-        if (c <= 512) LAUNCH((norm_backward<T, EIGHT, WIDE, 64, 1, 256>), groups, 256, lds, a);
-        else if (c <= 2048) LAUNCH((norm_backward<T, EIGHT, WIDE, 256, 1, 256>), groups, 256, lds, a);
-        else if (c <= 4096) LAUNCH((norm_backward<T, EIGHT, WIDE, 512, 1, 512>), groups, 512, lds, a);
-        else if (c <= 8192) LAUNCH((norm_backward<T, EIGHT, WIDE, 1024, 1, 1024>), groups, 1024, lds, a);
-        else if (c <= 16384) LAUNCH((norm_backward<T, EIGHT, WIDE, 1024, 2, 1024>), groups, 1024, lds, a);
-        else LAUNCH((norm_backward<T, EIGHT, WIDE, 1024, 4, 1024>), groups, 1024, lds, a);
+        if (c < 8) LAUNCH((norm_backward<T, EIGHT, 64, 1, 256, true>), groups, 256, lds, a);
+        else if (c <= 512) LAUNCH((norm_backward<T, EIGHT, 64, 1, 256>), groups, 256, lds, a);
+        else if (c <= 2048) LAUNCH((norm_backward<T, EIGHT, 256, 1, 256>), groups, 256, lds, a);
+        else if (c <= 4096) LAUNCH((norm_backward<T, EIGHT, 512, 1, 512>), groups, 512, lds, a);
+        else if (c <= 8192) LAUNCH((norm_backward<T, EIGHT, 1024, 1, 1024>), groups, 1024, lds, a);
+        else if (c <= 16384) LAUNCH((norm_backward<T, EIGHT, 1024, 2, 1024>), groups, 1024, lds, a);
+        else LAUNCH((norm_backward<T, EIGHT, 1024, 4, 1024>), groups, 1024, lds, a);
     } else {
-        if (c <= 512) LAUNCH((norm_backward<T, EIGHT, WIDE, 64, 1, 1024>), groups, 1024, lds, a);
-        else if (c <= 2048) LAUNCH((norm_backward<T, EIGHT, WIDE, 256, 1, 1024>), groups, 1024, lds, a);
-        else if (c <= 4096) LAUNCH((norm_backward<T, EIGHT, WIDE, 512, 1, 1024>), groups, 1024, lds, a);
-        else if (c <= 8192) LAUNCH((norm_backward<T, EIGHT, WIDE, 1024, 1, 1024>), groups, 1024, lds, a);
-        else if (c <= 16384) LAUNCH((norm_backward<T, EIGHT, WIDE, 1024, 2, 1024>), groups, 1024, lds, a);
-        else LAUNCH((norm_backward<T, EIGHT, WIDE, 1024, 4, 1024>), groups, 1024, lds, a);
+        if (c < 8) LAUNCH((norm_backward<T, EIGHT, 64, 1, 1024, true>), groups, 1024, lds, a);
+        else if (c <= 512) LAUNCH((norm_backward<T, EIGHT, 64, 1, 1024>), groups, 1024, lds, a);
+        else if (c <= 2048) LAUNCH((norm_backward<T, EIGHT, 256, 1, 1024>), groups, 1024, lds, a);
+        else if (c <= 4096) LAUNCH((norm_backward<T, EIGHT, 512, 1, 1024>), groups, 1024, lds, a);
+        else if (c <= 8192) LAUNCH((norm_backward<T, EIGHT, 1024, 1, 1024>), groups, 1024, lds, a);
+        else if (c <= 16384) LAUNCH((norm_backward<T, EIGHT, 1024, 2, 1024>), groups, 1024, lds, a);
+        else LAUNCH((norm_backward<T, EIGHT, 1024, 4, 1024>), groups, 1024, lds, a);
     }
     return TC_OK;
 }
@@ -242,17 +239,28 @@ int multiply(tc_ctx* ctx, ProductArgs a, float* part) {
     /* Up to sixteen rows: a pass over the weights alone, 1 x 4096 -> 4096 in 6.9 us against 10.5 by tiles.  Every workgroup reads all of x, though:
      * beyond eight rows, 16-bit weights that are past the caches' help go by tiles (16 x 4096 -> 11008: 18.4 us against 25.0). */
     const bool few = a.nq <= 8 || (a.nq <= 16 && (P_EIGHT || (uint64_t)a.np * a.nr <= 1u << 25));
-    if (FORWARD && few && pieces && in_pieces(a.p, a.nr, P_EIGHT, true) && in_pieces(a.q, a.nr, false, true))
-        return launch_product(ctx, product_thin<T, P_EIGHT, 8>, a, (a.np + 15) / 16, 512, 0);
+    if constexpr (FORWARD) {
+        if (few && in_pieces(a.p, a.nr, P_EIGHT, true) && in_pieces(a.q, a.nr, false, true))
+            return launch_product(ctx, product_thin<T, P_EIGHT, false, 8>, a, (a.np + 15) / 16, 512, 0);
+        if (few && a.nr >= 8) return launch_product(ctx, product_thin<T, P_EIGHT, true, 8>, a, (a.np + 15) / 16, 512, 0);
+    }
     const ProductPlan plan = product_plan(a.np, a.nq, a.nr);
-    if (!pieces) return launch_product(ctx, product<T, P_ALONG, P_EIGHT, Q_ALONG, FORWARD>, a, plan.tiles(128, 128), 256, 0);
     a.r_split = plan.r_split;
     if (plan.splits > 1) {
         a.part = part;
         a.ldp = plan.ldp;
     }
-    const uint64_t grid = plan.tiles(plan.side_p, plan.side_q) * plan.splits;
-    if (plan.side_p == 256) {
+    const uint64_t tiles = plan.tiles(plan.side, plan.side) * plan.splits, tiles128 = plan.tiles(128, 128) * plan.splits;
+    const size_t lds128 = 2 * 256 * 64 * 2, lds64 = 2 * 128 * 64 * 2;
+    if (!pieces) {
+        const uint64_t tiles64 = plan.tiles(64, 64) * plan.splits;
+        if ((P_ALONG ? a.nr : a.np) < 8 || (Q_ALONG ? a.nr : a.nq) < 8)
+            TRY(launch_product(ctx, product_paired<T, P_ALONG, P_EIGHT, Q_ALONG, FORWARD, 2, 64, 64, 2, 2>, a, tiles64, 256, lds64));
+        else if (plan.side > 64)
+            TRY(launch_product(ctx, product_paired<T, P_ALONG, P_EIGHT, Q_ALONG, FORWARD, 1, 128, 128, 2, 2>, a, tiles128, 256, lds128));
+        else
+            TRY(launch_product(ctx, product_paired<T, P_ALONG, P_EIGHT, Q_ALONG, FORWARD, 1, 64, 64, 2, 2>, a, tiles64, 256, lds64));
+    } else if (plan.side == 256) {
         if (P_EIGHT) {
             const uint32_t lines = P_ALONG ? a.np : a.nr, cols = P_ALONG ? a.nr : a.np;
             T* wide = (T*)((uint8_t*)part + plan.part_bytes());
@@ -264,11 +272,11 @@ int multiply(tc_ctx* ctx, ProductArgs a, float* part) {
         const size_t lds = 5 * 512 * 32 * 2;
         auto* kernel = product_deep<T, P_ALONG, Q_ALONG, FORWARD, 256, 256, 2, 4>;
         LARGE_LDS(kernel, lds);
-        TRY(launch_product(ctx, kernel, a, grid, 512, lds));
-    } else if (plan.side_p == 128) {
-        TRY(launch_product(ctx, product_paired<T, P_ALONG, P_EIGHT, Q_ALONG, FORWARD, 128, 128, 2, 2>, a, grid, 256, 2 * 256 * 64 * 2));
+        TRY(launch_product(ctx, kernel, a, tiles, 512, lds));
+    } else if (plan.side == 128) {
+        TRY(launch_product(ctx, product_paired<T, P_ALONG, P_EIGHT, Q_ALONG, FORWARD, 0, 128, 128, 2, 2>, a, tiles, 256, lds128));
     } else {
-        TRY(launch_product(ctx, product_paired<T, P_ALONG, P_EIGHT, Q_ALONG, FORWARD, 64, 64, 2, 2>, a, grid, 256, 2 * 128 * 64 * 2));
+        TRY(launch_product(ctx, product_paired<T, P_ALONG, P_EIGHT, Q_ALONG, FORWARD, 0, 64, 64, 2, 2>, a, tiles, 256, lds64));
     }
     if (plan.splits > 1) {
         const uint64_t pieces8 = (uint64_t)((a.np + 7) / 8) * a.nq;
@@ -282,21 +290,20 @@ int multiply(tc_ctx* ctx, ProductArgs a, float* part) {
 template <class T>
 int run_encode(tc_ctx* ctx, const tc_matrix* src, const tc_matrix* dst) {
     const RowArgs a{src->d_data, dst->d_data, dst->d_scale, src->ld, dst->ld, src->rows, src->cols};
-    return wide(src) && wide(dst) ? encode_rows<T, true>(ctx, a) : encode_rows<T, false>(ctx, a);
+    return encode_rows<T>(ctx, a);
 }
 template <class T>
 int run_decode(tc_ctx* ctx, const tc_matrix* src, const tc_matrix* dst) {
     const RowArgs a{src->d_data, dst->d_data, src->d_scale, src->ld, dst->ld, src->rows, src->cols};
     const dim3 grid((a.cols + 2047) / 2048, std::min<uint32_t>(a.rows, 65535));
-    if (wide(src) && wide(dst)) LAUNCH((checkpoint_decode<T, true>), grid, 256, 0, a);
+    if (a.cols < 8) LAUNCH((checkpoint_decode<T, true>), grid, 256, 0, a);
     else LAUNCH((checkpoint_decode<T, false>), grid, 256, 0, a);
     return TC_OK;
 }
 template <class T>
 int run_norm(tc_ctx* ctx, int kind, const tc_matrix* x, const void* gamma, const void* beta, float eps, const tc_matrix* y, float* mean, float* rstd) {
     const NormArgs a{x->d_data, x->dtype == TC_I8 ? x->d_scale : nullptr, gamma, beta, y->d_data, mean, rstd, x->ld, y->ld, x->rows, x->cols, eps, kind == TC_NORM_LAYER};
-    const bool w = wide(x) && wide(y) && (((uintptr_t)gamma | (uintptr_t)beta) & 15u) == 0;
-    return w ? norm_rows<T, true>(ctx, a) : norm_rows<T, false>(ctx, a);
+    return norm_rows<T>(ctx, a);
 }
 template <class T>
 int run_norm_backward(tc_ctx* ctx, int kind, const tc_matrix* dy, const tc_matrix* x, const void* gamma, const float* mean, const float* rstd,
@@ -305,9 +312,7 @@ int run_norm_backward(tc_ctx* ctx, int kind, const tc_matrix* dy, const tc_matri
     float* part = dgamma || dbeta ? (float*)ws : nullptr;
     const NormBackArgs a{dy->d_data, x->d_data, x->dtype == TC_I8 ? x->d_scale : nullptr, gamma, mean, rstd, dx ? dx->d_data : nullptr, part,
                          dy->ld, x->ld, dx ? dx->ld : 0, dy->rows, dy->cols, kind == TC_NORM_LAYER};
-    const bool w = wide(dy) && wide(x) && (!dx || wide(dx)) && ((uintptr_t)gamma & 15u) == 0;
-    if (a.scale) TRY((w ? norm_back_rows<T, true, true>(ctx, a, groups) : norm_back_rows<T, true, false>(ctx, a, groups)));
-    else TRY((w ? norm_back_rows<T, false, true>(ctx, a, groups) : norm_back_rows<T, false, false>(ctx, a, groups)));
+    TRY((a.scale ? norm_back_rows<T, true>(ctx, a, groups) : norm_back_rows<T, false>(ctx, a, groups)));
     return part ? sum_columns(ctx, part, 2 * (uint64_t)dy->cols, groups, dy->cols, dgamma, dbeta) : TC_OK;
 }
 template <class T>
@@ -326,7 +331,6 @@ int run_linear(tc_ctx* ctx, const tc_matrix* x, const tc_matrix* w, const void* 
     if (residual) { a.residual = residual->d_data; a.ldres = residual->ld; }
     if (z) { a.z = z->d_data; a.ldz = z->ld; }
     a.act = act;
-    a.wide_out = wide(y) && (!residual || wide(residual)) && (!z || wide(z)) && ((uintptr_t)bias & 15u) == 0;
     return a.p_scale ? multiply<T, true, true, true, true>(ctx, a, (float*)ws) : multiply<T, true, false, true, true>(ctx, a, (float*)ws);
 }
 template <class T>
@@ -347,14 +351,12 @@ int run_linear_backward(tc_ctx* ctx, const tc_matrix* dy, const tc_matrix* x, co
         SlopeArgs s = {};
         s.dy = dy->d_data;
         s.lddy = dy->ld;
-        bool wd = wide(dy);
         if (act != TC_ACT_NONE) {
             s.z = z->d_data;
             s.z_scale = z->dtype == TC_I8 ? z->d_scale : nullptr;
             s.ldz = z->ld;
             s.dz = dz->d_data;
             s.lddz = dz->ld;
-            wd = wd && wide(z) && wide(dz);
         }
         s.by_x = by_x ? base + plan.by_x : nullptr;
         s.by_w = by_w ? base + plan.by_w : nullptr;
@@ -368,7 +370,7 @@ int run_linear_backward(tc_ctx* ctx, const tc_matrix* dy, const tc_matrix* x, co
         s.act = act;
         const uint32_t groups = slope_groups(rows, out);
         const dim3 grid((out + 511) / 512, groups);
-        if (wd) LAUNCH((slopes<T, true>), grid, 256, 0, s);
+        if (out < 8) LAUNCH((slopes<T, true>), grid, 256, 0, s);
         else LAUNCH((slopes<T, false>), grid, 256, 0, s);
         if (dbias) TRY(sum_columns(ctx, s.part, out, groups, out, dbias, nullptr));
     }
@@ -382,7 +384,6 @@ int run_linear_backward(tc_ctx* ctx, const tc_matrix* dy, const tc_matrix* x, co
         a.nr = out;
         a.out = dx->d_data;
         a.ldo = dx->ld;
-        a.wide_out = wide(dx);
         a.factor = by_w && m ? m + 2 : nullptr;
         TRY((by_w ? multiply<T, false, true, true, false>(ctx, a, parts) : multiply<T, false, false, true, false>(ctx, a, parts)));
     }
@@ -395,7 +396,6 @@ int run_linear_backward(tc_ctx* ctx, const tc_matrix* dy, const tc_matrix* x, co
         a.nr = rows;
         a.out = dw->d_data;
         a.ldo = dw->ld;
-        a.wide_out = wide(dw);
         a.factor = by_x ? m : nullptr;
         TRY((by_x ? multiply<T, false, true, false, false>(ctx, a, parts) : multiply<T, false, false, false, false>(ctx, a, parts)));
     }

@@ -65,7 +65,8 @@ def ok(got, want, bound):
 # ---- checkpoints ---------------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("rows,cols,pad", [(1, 1, (0, 0)), (3, 7, (0, 0)), (5, 8, (8, 8)), (9, 512, (0, 0)), (4, 513, (0, 3)), (2, 2048, (1, 0)), (7, 4096, (0, 0)),
-                                           (3, 4104, (0, 0)), (2, 11008, (0, 0)), (2, 16384, (0, 8)), (2, 16385, (0, 0)), (2, 40000, (0, 0)), (1000, 64, (0, 0))])
+                                           (3, 4104, (0, 0)), (2, 11008, (0, 0)), (2, 16384, (0, 8)), (2, 16385, (0, 0)), (2, 40000, (0, 0)), (1000, 64, (0, 0)),
+                                           (3, 9, (0, 0)), (2, 2049, (0, 0)), (2, 4101, (5, 0)), (2, 8199, (0, 0)), (3, 1, (0, 2)), (2, 18433, (0, 0))])
 def test_checkpoints(T, ctx, dtype, rows, cols, pad):
     t = ref.DT[dtype]
     _, x = strided(rand((rows, cols), rows * cols, t, 3.0), *pad)
@@ -109,7 +110,8 @@ def test_checkpoint_values_at_the_edges(T, ctx, dtype):
 
 # ---- norms ---------------------------------------------------------------------------------------------------------
 NORM_SIZES = [(1, 1, (0, 0)), (1, 4096, (0, 0)), (3, 7, (0, 0)), (6, 512, (8, 0)), (5, 520, (0, 0)), (33, 1027, (0, 2)), (4, 2056, (0, 0)), (17, 4096, (0, 0)),
-              (3, 8192, (0, 0)), (2, 11008, (0, 0)), (2, 16392, (0, 0)), (2, 32768, (0, 0)), (2, 32767, (0, 0)), (1500, 256, (0, 0)), (700, 1024, (0, 0))]
+              (3, 8192, (0, 0)), (2, 11008, (0, 0)), (2, 16392, (0, 0)), (2, 32768, (0, 0)), (2, 32767, (0, 0)), (1500, 256, (0, 0)), (700, 1024, (0, 0)),
+              (2, 9, (0, 0)), (3, 515, (0, 0)), (2, 2049, (1, 0)), (1100, 4099, (0, 0)), (2, 8197, (0, 0)), (1030, 7, (0, 0)), (2, 16390, (0, 0))]
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
@@ -201,7 +203,9 @@ def test_norm_of_rows_that_are_not_numbers(T, ctx, dtype):
 # ---- products ------------------------------------------------------------------------------------------------------
 LINEAR_SIZES = [(1, 1, 1, (0, 0)), (1, 64, 128, (0, 0)), (1, 4096, 264, (0, 0)), (2, 65, 7, (0, 0)), (3, 63, 130, (1, 0)), (15, 1000, 48, (0, 0)), (16, 512, 96, (8, 8)),
                 (17, 72, 129, (0, 0)), (33, 256, 1000, (0, 0)), (64, 200, 64, (0, 0)), (65, 1027, 33, (0, 0)), (100, 8, 8, (0, 0)), (127, 128, 256, (0, 0)),
-                (129, 640, 264, (0, 0)), (257, 64, 520, (0, 5)), (300, 328, 392, (0, 0)), (512, 1024, 512, (0, 0))]
+                (129, 640, 264, (0, 0)), (257, 64, 520, (0, 5)), (300, 328, 392, (0, 0)), (512, 1024, 512, (0, 0)),
+                # a strip of 512 columns, a tile, a chunk or a piece with one to seven entries in it
+                (9, 24, 515, (0, 0)), (5, 1025, 1030, (0, 0)), (70, 129, 513, (3, 0)), (3, 9, 1031, (0, 0)), (131, 519, 65, (0, 1))]
 
 
 def linear_inputs(T, t, rows, k, n, w8, seed, pad):
