@@ -156,34 +156,18 @@ __device__ __forceinline__ void to_front(uint32_t (&w)[2], uint32_t count) {
     w[0] = __builtin_amdgcn_alignbit(w[1], w[0], s);
     w[1] >>= s;
 }
-/* the eight entries from p on, of which `count` (up to 8) belong to the row and the rest is to be moved away by to_front; SHORT: read one by one, as the row may have fewer than eight */
-template <bool SHORT>
+/* the first `count` of the eight entries from p on, one by one, zeros behind them: for rows that have fewer than eight */
 __device__ __forceinline__ void read_piece(const uint16_t* p, uint32_t count, uint32_t (&w)[4]) {
     w[0] = w[1] = w[2] = w[3] = 0;
-    if (SHORT) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if ((uint32_t)j < count) w[j >> 1] |= (uint32_t)p[j] << (j & 1) * 16;
-    } else if (count) {
-        const uint4 x = unaligned<uint4>(p + (int)count - 8);
-        w[0] = x.x;
-        w[1] = x.y;
-        w[2] = x.z;
-        w[3] = x.w;
-    }
+    for (int j = 0; j < 8; ++j)
+        if ((uint32_t)j < count) w[j >> 1] |= (uint32_t)p[j] << (j & 1) * 16;
 }
-template <bool SHORT>
 __device__ __forceinline__ void read_piece(const uint8_t* p, uint32_t count, uint32_t (&w)[2]) {
     w[0] = w[1] = 0;
-    if (SHORT) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if ((uint32_t)j < count) w[j >> 2] |= (uint32_t)p[j] << (j & 3) * 8;
-    } else if (count) {
-        const uint2 x = unaligned<uint2>(p + (int)count - 8);
-        w[0] = x.x;
-        w[1] = x.y;
-    }
+    for (int j = 0; j < 8; ++j)
+        if ((uint32_t)j < count) w[j >> 2] |= (uint32_t)p[j] << (j & 3) * 8;
 }
 template <int TH>
 __device__ __forceinline__ uint32_t row_col(int t, int c) { return ((uint32_t)c * TH + t) * 8; }
@@ -194,7 +178,7 @@ struct Raw {
     __device__ __forceinline__ void load(const T* p, int t, int c, uint32_t cols) {
         const uint32_t k = row_col<TH>(t, c);
         if (SHORT) {
-            read_piece<true>((const uint16_t*)p + k, entries_at(k, cols), w);
+            read_piece((const uint16_t*)p + k, entries_at(k, cols), w);
             return;
         }
         uint4 x = make_uint4(0, 0, 0, 0);
@@ -223,7 +207,7 @@ struct RawQ {
     __device__ __forceinline__ void load(const int8_t* p, int t, int c, uint32_t cols) {
         const uint32_t k = row_col<TH>(t, c);
         if (SHORT) {
-            read_piece<true>((const uint8_t*)p + k, entries_at(k, cols), w);
+            read_piece((const uint8_t*)p + k, entries_at(k, cols), w);
             return;
         }
         uint2 x = make_uint2(0, 0);
@@ -848,50 +832,67 @@ template <class T, bool ALONG, bool EIGHT, int LOOSE, int SIDE, int TH, int BK>
 struct Feed {
     typedef Tile<T, ALONG, SIDE, BK> tile;
     static constexpr int N = SIDE * BK / 8 / TH, PIECES = ALONG ? BK / 8 : SIDE / 8, SIZE = EIGHT ? 1 : 2;
-    static constexpr bool HELD = EIGHT || LOOSE != 0, SHORT = LOOSE == 2;
+    static constexpr bool HELD = EIGHT || LOOSE != 0;
     static constexpr uint32_t NOWHERE = 0x80000000u;
-    typedef uint32_t Held[HELD ? N : 1][EIGHT ? 2 : 4];
+    typedef typename std::conditional<EIGHT, uint2, uint4>::type Piece;
+    typedef Piece Held[HELD ? N : 1];
     typename std::conditional<LOOSE != 0, uint64_t, uint32_t>::type off[N];
-    uint32_t have[LOOSE ? N : 1];    /* entries of a piece that the operand has, as far as the axis across the sum says */
-    uint32_t count[LOOSE ? N : 1];   /* entries of the pieces in `held` */
-    bool ragged;                     /* some of them are not whole (the same for all lanes) */
     const char* base;
-    uint64_t step;
-    uint32_t nr, line_bytes;
+    uint64_t step, ld;
+    uint32_t nr, line_bytes, left;   /* left: of the operand's axis across the sum, from this tile on */
+    uint32_t held_rest;              /* of the sum, from the tile in `held` on */
+    __device__ static __forceinline__ int line_of(int n) { return n / PIECES; }
     __device__ static __forceinline__ int piece_of(int n) {
         const int line = n / PIECES, slot = n % PIECES;
         return ALONG ? slot ^ tile::turn(line) : ((slot >> 1) ^ tile::spread(line)) << 1 | (slot & 1);
     }
+    /* LOOSE: how far before its place piece n has to be read to end with its row, `rest` of the sum being left; eight or more: nothing of it is the row's */
+    __device__ __forceinline__ uint32_t back(int n, uint32_t rest) const {
+        const uint32_t end = piece_of(n) * 8 + 8, has = ALONG ? rest : left;
+        return end > has ? end - has : 0;
+    }
     /* r from `r0` on, `nr_` of them */
     __device__ __forceinline__ void init(const Operand& o, uint64_t side0, uint32_t sides, uint32_t r0, uint32_t nr_, int t) {
         nr = nr_;
+        ld = o.ld;
+        left = sides - (uint32_t)side0;
         line_bytes = (uint32_t)(o.ld * SIZE);
         base = (const char*)o.d + (ALONG ? side0 * o.ld + r0 : r0 * o.ld + side0) * SIZE;
         step = ALONG ? BK * SIZE : BK * o.ld * SIZE;
-        ragged = !ALONG && sides - side0 < SIDE && sides % 8;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int n = i * TH + t, line = n / PIECES, piece = piece_of(n);
-            const uint64_t side = side0 + (ALONG ? line : piece * 8);
-            if (LOOSE) {
-                off[i] = (line * o.ld + piece * 8) * SIZE;
-                have[i] = side >= sides ? 0 : ALONG || sides - side >= 8 ? 8 : (uint32_t)(sides - side);
-            } else off[i] = side < sides ? line * line_bytes + piece * 8 * SIZE : NOWHERE;
+            const int n = i * TH + t, line = line_of(n), piece = piece_of(n);
+            const bool in = (uint32_t)(ALONG ? line : piece * 8) < left;
+            if (LOOSE) off[i] = ((ALONG && !in ? 0 : line) * o.ld + piece * 8) * SIZE;        /* a line too many reads the first one: its results are dropped */
+            else off[i] = in ? line * line_bytes + piece * 8 * SIZE : NOWHERE;
         }
     }
-    /* tile number k, to its place in LDS or into `held`; past the last one: zeros */
+    /* tile number k, to its place in LDS or into `held`; past the last one: zeros (LOOSE: nothing) */
     __device__ __forceinline__ void issue(T* lds, Held& held, uint32_t k, int t) {
         const uint32_t rest = __builtin_amdgcn_readfirstlane(nr > k * BK ? nr - k * BK : 0);      /* a saturating difference, which is a vector instruction */
         const char* at = base + (rest ? k * step : 0);
-        if constexpr (LOOSE) {
-            typedef typename std::conditional<EIGHT, uint8_t, uint16_t>::type entry;
-            if (ALONG) ragged = rest < BK && rest % 8;
+        if constexpr (LOOSE == 1) {
+            held_rest = rest;
+            if (!rest) return;
+            /* no load depends on a condition: pieces past an end are read where the row's last eight entries are, or from its last line, and put right by settle() */
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 const int n = i * TH + t;
-                const uint32_t r = ALONG ? piece_of(n) * 8 : n / PIECES, left = rest > r ? rest - r : 0;
-                count[i] = ALONG ? (left < have[i] ? left : have[i]) : (left ? have[i] : 0);
-                read_piece<SHORT>((const entry*)(at + off[i]), count[i], held[i]);
+                int64_t o = (int64_t)off[i] - (int64_t)back(n, rest) * SIZE;
+                if (!ALONG && rest < BK && (uint32_t)line_of(n) >= rest) o -= (int64_t)(line_of(n) - (rest - 1)) * (int64_t)ld * SIZE;
+                held[i] = unaligned<Piece>(at + o);
+            }
+        } else if constexpr (LOOSE == 2) {
+            /* rows shorter than eight entries: one by one */
+            typedef typename std::conditional<EIGHT, uint8_t, uint16_t>::type entry;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int n = i * TH + t;
+                const uint32_t b = back(n, rest);
+                const bool live = b < 8 && (ALONG ? (uint32_t)line_of(n) < left : (uint32_t)line_of(n) < rest);
+                uint32_t w[EIGHT ? 2 : 4];
+                read_piece((const entry*)(at + off[i]), live ? 8 - b : 0, w);
+                held[i] = __builtin_bit_cast(Piece, w);
             }
         } else {
             const uint32_t span = ALONG ? NOWHERE - 1 : (rest < BK ? rest : BK) * line_bytes;
@@ -905,28 +906,32 @@ struct Feed {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 uint32_t o = off[i];
-                if constexpr (EIGHT) {
-                    const auto x = __builtin_amdgcn_raw_buffer_load_b64(r, o, 0, 0);
-                    held[i][0] = x[0];
-                    held[i][1] = x[1];
-                } else
+                if constexpr (EIGHT) held[i] = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(r, o, 0, 0));
+                else
                     __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(lds + (i * TH + (t & ~63)) * 8), 16, o, 0, 0, 0);
             }
         }
     }
     __device__ __forceinline__ void settle(T* lds, Held& held, int t) {
         if constexpr (HELD) {
-            if (LOOSE == 1 && ragged) {
-                asm volatile("");        /* a branch */
-#pragma unroll
-                for (int i = 0; i < N; ++i)
-                    if (count[i] && count[i] < 8) to_front(held[i], count[i]);
-            }
+            /* the same for all lanes: whether this tile has pieces that issue() could not read where they are */
+            const bool ragged = LOOSE == 1 && (held_rest < BK || (!ALONG && left < SIDE && left % 8));
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 typename Vec<T>::v8* to = (typename Vec<T>::v8*)(lds + (i * TH + t) * 8);
-                if constexpr (EIGHT) *to = widen<T>(held[i][0], held[i][1]);
-                else *to = __builtin_bit_cast(typename Vec<T>::v8, make_uint4(held[i][0], held[i][1], held[i][2], held[i][3]));
+                uint32_t w[EIGHT ? 2 : 4];
+                __builtin_memcpy(w, &held[i], sizeof w);
+                if (LOOSE == 1 && ragged) {
+                    asm volatile("");    /* a branch */
+                    const int n = i * TH + t;
+                    const uint32_t b = back(n, held_rest);
+                    if (b >= 8 || (!ALONG && (uint32_t)line_of(n) >= held_rest))
+#pragma unroll
+                        for (uint32_t& x : w) x = 0;
+                    else if (b) to_front(w, 8 - b);
+                }
+                if constexpr (EIGHT) *to = widen<T>(w[0], w[1]);
+                else *to = __builtin_bit_cast(typename Vec<T>::v8, make_uint4(w[0], w[1], w[2], w[3]));
             }
         }
     }
@@ -1094,8 +1099,9 @@ __global__ __launch_bounds__(256) void join_parts(const ProductArgs a, uint32_t 
  * y = x w^T for at most sixteen rows of x: the weights are read once and that is all it costs.  A workgroup has sixteen of w's rows and its waves share r; each goes from memory
  * straight into the matrix instruction: lane l takes 16 r of row l & 15, from 16 (l >> 4) on, the first eight of them for one
  * instruction and the last eight for the next (any order of r does, if both operands have the same).  The waves' sums are added in order.
- * A wave has AHEAD chunks of 64 r under way.  LOOSE: rows of any alignment and of any length from eight on. */
-template <class T, bool EIGHT, bool LOOSE, int WAVES>
+ * A wave has four chunks of 64 r under way.  Sixteen waves where the weights are int8 and their rows therefore short (1 x 4096 -> 11008, cold:
+ * 13.3 us; eight waves 15.3), eight otherwise.  Rows of whole, aligned pieces of sixteen. */
+template <class T, bool EIGHT, int WAVES>
 __global__ __launch_bounds__(WAVES * 64) void product_thin(const ProductArgs a) {
     typedef typename Vec<T>::v8 v8;
     __shared__ float sums[WAVES][256];
@@ -1105,62 +1111,37 @@ __global__ __launch_bounds__(WAVES * 64) void product_thin(const ProductArgs a) 
     constexpr uint32_t NOWHERE = 0x80000000u;
     const bool has_p = p0 + line < a.np, has_q = line < a.nq;
     f4 acc = {0, 0, 0, 0};
-    constexpr int AHEAD = EIGHT ? 8 : 4;
+    constexpr int AHEAD = 4;
     const uint32_t chunks = (a.nr + 63) / 64;
     for (uint32_t c = w; c < chunks; c += WAVES * AHEAD) {
         uint32_t x[AHEAD][2][WORDS], y[AHEAD][2][4];
-        if constexpr (LOOSE) {
-            const char* rp = (const char*)a.p.d + (has_p ? p0 + line : p0) * a.p.ld * SIZE;
-            const char* rq = (const char*)a.q.d + (has_q ? line : 0) * a.q.ld * 2;
-            typedef typename std::conditional<EIGHT, uint8_t, uint16_t>::type entry;
+        const __amdgpu_buffer_rsrc_t rp = __builtin_amdgcn_make_buffer_rsrc((char*)a.p.d + p0 * a.p.ld * SIZE, 0, NOWHERE - 1, 0x00020000);
+        const __amdgpu_buffer_rsrc_t rq = __builtin_amdgcn_make_buffer_rsrc((void*)a.q.d, 0, NOWHERE - 1, 0x00020000);
+        const uint32_t op = (uint32_t)(line * a.p.ld + at) * SIZE, oq = (uint32_t)(line * a.q.ld + at) * 2;
 #pragma unroll
-            for (int i = 0; i < AHEAD; ++i)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const uint32_t r = (c + i * WAVES) * 64 + at + h * 8, n = entries_at(r, a.nr);
-                    read_piece<false>((const entry*)rp + r, has_p ? n : 0, x[i][h]);
-                    read_piece<false>((const uint16_t*)rq + r, has_q ? n : 0, y[i][h]);
-                }
-#pragma unroll
-            for (int i = 0; i < AHEAD; ++i)
-                if ((c + i * WAVES) * 64 + 64 > a.nr)          /* the last chunk */
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const uint32_t n = entries_at((c + i * WAVES) * 64 + at + h * 8, a.nr);
-                        if (n && n < 8) {
-                            to_front(x[i][h], n);
-                            to_front(y[i][h], n);
-                        }
-                    }
-        } else {
-            const __amdgpu_buffer_rsrc_t rp = __builtin_amdgcn_make_buffer_rsrc((char*)a.p.d + p0 * a.p.ld * SIZE, 0, NOWHERE - 1, 0x00020000);
-            const __amdgpu_buffer_rsrc_t rq = __builtin_amdgcn_make_buffer_rsrc((void*)a.q.d, 0, NOWHERE - 1, 0x00020000);
-            const uint32_t op = (uint32_t)(line * a.p.ld + at) * SIZE, oq = (uint32_t)(line * a.q.ld + at) * 2;
-#pragma unroll
-            for (int i = 0; i < AHEAD; ++i) {
-                const uint32_t r = (c + i * WAVES) * 64, from = r < a.nr ? r : 0;
-                const bool in = r + at < a.nr;                 /* the rows are whole pieces of sixteen */
-                const auto one = __builtin_amdgcn_raw_buffer_load_b128(rp, in && has_p ? op : NOWHERE, from * SIZE, 0);
-                if constexpr (EIGHT) {
-                    x[i][0][0] = one[0];
-                    x[i][0][1] = one[1];
-                    x[i][1][0] = one[2];
-                    x[i][1][1] = one[3];
-                } else {
-                    const auto two = __builtin_amdgcn_raw_buffer_load_b128(rp, in && has_p ? op + 16 : NOWHERE, from * SIZE, 0);
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        x[i][0][k] = one[k];
-                        x[i][1][k] = two[k];
-                    }
-                }
-                const auto lo = __builtin_amdgcn_raw_buffer_load_b128(rq, in && has_q ? oq : NOWHERE, from * 2, 0);
-                const auto hi = __builtin_amdgcn_raw_buffer_load_b128(rq, in && has_q ? oq + 16 : NOWHERE, from * 2, 0);
+        for (int i = 0; i < AHEAD; ++i) {
+            const uint32_t r = (c + i * WAVES) * 64, from = r < a.nr ? r : 0;
+            const bool in = r + at < a.nr;                 /* the rows are whole pieces of sixteen */
+            const auto one = __builtin_amdgcn_raw_buffer_load_b128(rp, in && has_p ? op : NOWHERE, from * SIZE, 0);
+            if constexpr (EIGHT) {
+                x[i][0][0] = one[0];
+                x[i][0][1] = one[1];
+                x[i][1][0] = one[2];
+                x[i][1][1] = one[3];
+            } else {
+                const auto two = __builtin_amdgcn_raw_buffer_load_b128(rp, in && has_p ? op + 16 : NOWHERE, from * SIZE, 0);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    y[i][0][k] = lo[k];
-                    y[i][1][k] = hi[k];
+                    x[i][0][k] = one[k];
+                    x[i][1][k] = two[k];
                 }
+            }
+            const auto lo = __builtin_amdgcn_raw_buffer_load_b128(rq, in && has_q ? oq : NOWHERE, from * 2, 0);
+            const auto hi = __builtin_amdgcn_raw_buffer_load_b128(rq, in && has_q ? oq + 16 : NOWHERE, from * 2, 0);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                y[i][0][k] = lo[k];
+                y[i][1][k] = hi[k];
             }
         }
 #pragma unroll

@@ -240,9 +240,9 @@ int multiply(tc_ctx* ctx, ProductArgs a, float* part) {
      * beyond eight rows, 16-bit weights that are past the caches' help go by tiles (16 x 4096 -> 11008: 18.4 us against 25.0). */
     const bool few = a.nq <= 8 || (a.nq <= 16 && (P_EIGHT || (uint64_t)a.np * a.nr <= 1u << 25));
     if constexpr (FORWARD) {
+        constexpr int waves = P_EIGHT ? 16 : 8;
         if (few && in_pieces(a.p, a.nr, P_EIGHT, true) && in_pieces(a.q, a.nr, false, true))
-            return launch_product(ctx, product_thin<T, P_EIGHT, false, 8>, a, (a.np + 15) / 16, 512, 0);
-        if (few && a.nr >= 8) return launch_product(ctx, product_thin<T, P_EIGHT, true, 8>, a, (a.np + 15) / 16, 512, 0);
+            return launch_product(ctx, product_thin<T, P_EIGHT, waves>, a, (a.np + 15) / 16, waves * 64, 0);
     }
     const ProductPlan plan = product_plan(a.np, a.nq, a.nr);
     a.r_split = plan.r_split;
