@@ -243,7 +243,7 @@ int tc_encode_batch_scaled(tc_ctx* ctx, int count, const void* const* d_src, con
 
 /* A view of device memory: rows x cols elements, row r at d_data + r * ld elements.  d_scale: for TC_I8, one float32 for
  * each row, the entry standing for d_scale[r] * q; not looked at for the other types.  Any alignment of whole elements
- * and any ld >= cols will do; 16-byte aligned rows of a multiple of 8 elements are what the kernels are fast on.
+ * and any ld >= cols will do; products are fastest where rows lie on 16 bytes (int8: 8) and have a multiple of 8 elements, up to 2^21 apart.
  * What lies between the rows (cols .. ld - 1) is neither read as data nor written.  rows = 0 is an empty view (d_data may be NULL). */
 typedef struct tc_matrix {
     void* d_data;
@@ -265,6 +265,7 @@ int tc_checkpoint_encode(tc_ctx* ctx, const tc_matrix* src, const tc_matrix* dst
 int tc_checkpoint_decode(tc_ctx* ctx, const tc_matrix* src, const tc_matrix* dst);
 
 /* Norms over the last axis.  TC_NORM_LAYER: mu the mean, rstd = 1 / sqrt(mean((x - mu)^2) + eps); TC_NORM_RMS: mu = 0.
+ * Squares are formed in float32, so entries beyond 1e18 (bfloat16 has them) overflow.
  * y = (x - mu) rstd gamma + beta.  x: 16 bits, or TC_I8 (a checkpoint, whose norm is recomputed); y: 16 bits; d_gamma, d_beta: cols values of
  * y's type, either may be NULL (1, 0).  d_mean, d_rstd: rows float32 each, for the backward pass, or NULL.  0 < eps < 1. */
 #define TC_NORM_LAYER 0

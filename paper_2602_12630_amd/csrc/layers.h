@@ -13,16 +13,14 @@ namespace layers {
 
 typedef float f4 __attribute__((ext_vector_type(4)));
 template <class T> struct Vec {
-    typedef T v4 __attribute__((ext_vector_type(4)));
     typedef T v8 __attribute__((ext_vector_type(8)));
 };
-typedef int8_t q8 __attribute__((ext_vector_type(8)));
 
 /* ---- activations: value and slope ------------------------------------------------------------------
  * Phi(z) by the rational form 7.1.26 of Abramowitz and Stegun's handbook: the upper tail of the normal distribution is
  * t (a1 + t (a2 + ..)) exp(-z^2 / 2) / 2 with t = 1 / (1 + p |z| / sqrt 2), within 7.5e-8 of it everywhere, which is the
  * size of a float32 rounding of Phi.  gelu = max(z, 0) - |z| tail: some 22 operations, where the library's erf alone takes 40; in the epilogue
- * of a product of 8192 x 4096 -> 11008 they cost what is left in DESIGN_GELU.  |z| is held at 14, beyond which every factor has
+ * of a product of 8192 x 4096 -> 11008 they add some 60 us to 640.  |z| is held at 14, beyond which every factor has
  * become 0, so that infinities (values before the activation that overflowed) do not turn into NaNs; NaNs stay. */
 __device__ __forceinline__ float held_at_14(float z) {
     const float a = fabsf(z);
@@ -273,7 +271,7 @@ struct RowArgs {
  * number: rounding it, half to even, is then rounding t / amax.  Added to 1.5 * 2^23 its low byte is q.
  * Rows with infinities or NaNs, or an amax out of the range of these scalings, take the careful way: q from the whole number next to the quotient by the
  * sign of the remainder t - q amax.
- * Bound by memory: 8192 x 11008 in SPEED_ENCODE.  Rows longer than the registers hold (NCH = 0) are read twice. */
+ * Bound by memory, some ten operations an entry: 8192 x 11008 in 58 us, 4.7 GB a millisecond (29 operations an entry, the careful way for all: 107 us).  Rows longer than the registers hold (NCH = 0) are read twice. */
 __device__ __forceinline__ float quantised(float x, float amax, float inv, int e) {
     const float t = 127.0f * ldexpf(x, e);
     float q = rintf(t * inv);
@@ -375,7 +373,8 @@ __global__ __launch_bounds__(256) void checkpoint_decode(const RowArgs a) {
 }
 
 /* ---- norms --------------------------------------------------------------------------------------------
- * A row is read once and stays in registers: its mean, then the mean square about it (no difference of large sums), then y. */
+ * A row is read once and stays in registers: its mean, then the mean square about it (no difference of large sums), then y.
+ * Short calls are launches (one row of 4096: 2.3 us in the kernel, 4.4 a call); 487 x 4096 4.3 us. */
 struct NormArgs {
     const void* x;
     const float* scale;              /* x is int8 where this is set */
@@ -471,8 +470,8 @@ __global__ __launch_bounds__(TH < 256 ? 256 : TH) void norm_forward(const NormAr
 
 /* The gradient: a workgroup of LANES lanes takes LANES / TH rows at a time and every gridDim-th such set; a lane keeps the sums of dy xh and dy
  * for its columns over all of them, so that gamma's and beta's gradients cost one partial row per workgroup and no second
- * pass over the activations.  The next set's loads are under way while this one's two sums are formed, at one barrier a set (the cells
- * alternate).  The row sets of a workgroup are added in order through LDS; column_sums adds the workgroups. */
+ * pass over the activations.  The next two sets' loads are under way while this one's two sums are formed, at one barrier a set.  The row sets of a workgroup are added in order through LDS; column_sums adds the workgroups.
+ * Bound by memory: 16384 x 4096 from int8 rows in 82 us, 335 MB, 4.1 GB a millisecond (copies reach 5.2). */
 struct NormBackArgs {
     const void *dy, *x;
     const float* scale;
@@ -488,7 +487,7 @@ template <class T, bool EIGHT, int TH, int NCH, int LANES, bool SHORT = false>
 __global__ __launch_bounds__(LANES) void norm_backward(const NormBackArgs a) {
     extern __shared__ float lds[];
     constexpr int SETS = LANES / TH;
-    __shared__ float2 cells[2][16];
+    __shared__ float2 cells[3][16];
     const int t = threadIdx.x % TH, set = threadIdx.x / TH;
     float dg[NCH][8], db[NCH][8];
 #pragma unroll
@@ -504,8 +503,8 @@ __global__ __launch_bounds__(LANES) void norm_backward(const NormBackArgs a) {
         }
     const float per = 1.0f / (float)a.cols;
     const uint64_t step = (uint64_t)gridDim.x * SETS;
-    /* A row is kept as it was read and unpacked twice, for the sums and for dx: two rows' raw bits take fewer registers than one row's values.
-     * Where a lane has more than one chunk of a row there is no room for the next one. */
+    /* A row is kept as it was read and unpacked twice, for the sums and for dx: three rows' raw bits take fewer registers than one row's values (values kept across the barrier spilled: 16384 x 4096 in 175 us).
+     * Where a lane has more than one chunk of a row there is no room for the next ones. */
     constexpr bool AHEAD = NCH == 1;
     typedef typename std::conditional<EIGHT, RawQ<TH, SHORT>, Raw<T, TH, SHORT>>::type RawX;
     struct Row {
@@ -561,25 +560,26 @@ __global__ __launch_bounds__(LANES) void norm_backward(const NormBackArgs a) {
             store8<T, TH>((T*)a.dx + row * a.lddx, t, c, cols, v);
         }
     };
-    float2 *cell0 = cells[0] + set * (TH / 64), *cell1 = cells[1] + set * (TH / 64);
-    /* every lane of the workgroup makes the same rounds */
+    /* every lane of the workgroup makes the same rounds; the cells go round by three, so one barrier a round is enough */
     const uint64_t begin = (uint64_t)blockIdx.x * SETS;
     if constexpr (AHEAD) {
-        Row one, two;
-        fetch(one, begin + set);
-        for (uint64_t first = begin; first < a.rows; first += 2 * step) {
-            fetch(two, first + step + set);
-            work(one, first + set, cell0);
-            if (first + step >= a.rows) break;
-            fetch(one, first + 2 * step + set);
-            work(two, first + step + set, cell1);
+        Row rows[3];
+        fetch(rows[0], begin + set);
+        fetch(rows[1], begin + step + set);
+        for (uint64_t first = begin; first < a.rows; first += 3 * step) {
+#pragma unroll
+            for (int i = 0; i < 3; ++i) {
+                if (first + i * step >= a.rows) break;
+                fetch(rows[(i + 2) % 3], first + (i + 2) * step + set);
+                work(rows[i], first + i * step + set, cells[i] + set * (TH / 64));
+            }
         }
     } else {
         Row one;
         int turn = 0;
         for (uint64_t first = begin; first < a.rows; first += step, turn ^= 1) {
             fetch(one, first + set);
-            work(one, first + set, turn ? cell1 : cell0);
+            work(one, first + set, cells[turn] + set * (TH / 64));
         }
     }
     if (!a.part) return;

@@ -5,6 +5,7 @@
  * launches, which only CPU tests of the checks and of the views use.
  */
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <type_traits>
 
@@ -227,12 +228,15 @@ int launch_product(tc_ctx* ctx, K* kernel, const ProductArgs& a, uint64_t grid, 
     LAUNCH(kernel, (uint32_t)grid, threads, lds, a);
     return TC_OK;
 }
-/* kernels that use more than the 64 KB of LDS that every kernel may */
-#define LARGE_LDS(kernel, bytes)                                                                                                     \
-    do {                                                                                                                             \
-        static const int e_ = (int)hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)(bytes)); \
-        if (e_) return ctx_fail_hip(ctx, e_, "LDS of a product");                                                                    \
-    } while (0)
+/* A kernel that uses more than the 64 KB of LDS that every kernel may has to say so once on each GPU; `said` has a bit for each. */
+int allow_lds(tc_ctx* ctx, const void* kernel, size_t bytes, std::atomic<uint64_t>& said) {
+    const uint64_t bit = 1ull << (ctx_device(ctx) & 63);
+    if (said.load(std::memory_order_relaxed) & bit) return TC_OK;
+    int e = (int)hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (e) return ctx_fail_hip(ctx, e, "LDS of a product");
+    said.fetch_or(bit, std::memory_order_relaxed);
+    return TC_OK;
+}
 template <class T, bool P_ALONG, bool P_EIGHT, bool Q_ALONG, bool FORWARD>
 int multiply(tc_ctx* ctx, ProductArgs a, float* part) {
     const bool pieces = in_pieces(a.p, P_ALONG ? a.nr : a.np, P_EIGHT) && in_pieces(a.q, Q_ALONG ? a.nr : a.nq, false);
@@ -271,7 +275,8 @@ int multiply(tc_ctx* ctx, ProductArgs a, float* part) {
         }
         const size_t lds = 5 * 512 * 32 * 2;
         auto* kernel = product_deep<T, P_ALONG, Q_ALONG, FORWARD, 256, 256, 2, 4>;
-        LARGE_LDS(kernel, lds);
+        static std::atomic<uint64_t> said{0};
+        TRY(allow_lds(ctx, (const void*)kernel, lds, said));
         TRY(launch_product(ctx, kernel, a, tiles, 512, lds));
     } else if (plan.side == 128) {
         TRY(launch_product(ctx, product_paired<T, P_ALONG, P_EIGHT, Q_ALONG, FORWARD, 0, 128, 128, 2, 2>, a, tiles, 256, lds128));

@@ -177,6 +177,7 @@ static int fail_hip(tc_ctx* ctx, int e, const char* where) {
 
 namespace tc {
 rt::stream_t ctx_stream(const tc_ctx* ctx) { return ctx->stream; }
+int ctx_device(const tc_ctx* ctx) { return ctx->device; }
 int ctx_use_device(tc_ctx* ctx) {
     RT(rt::set_device(ctx->device));
     return TC_OK;

@@ -396,6 +396,22 @@ def test_a_row_that_is_not_a_number_stays_alone(T, ctx, dtype):
         assert torch.isnan(dx[4]).all() and torch.isnan(dx).sum() == k and torch.isnan(dw[9]).all() and torch.isnan(dw).sum() == k
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,k,n", [(3, 64, 48), (70, 72, 65), (3, 65, 33)])
+def test_the_smallest_values_are_not_lost(T, ctx, dtype, rows, k, n):
+    """entries below the type's normal range, in products by one: the results are they themselves"""
+    t = ref.DT[dtype]
+    least = torch.finfo(t).smallest_normal * torch.finfo(t).eps
+    x = (torch.arange(rows * k, device="cuda").reshape(rows, k) % 15 - 7).double() * least
+    x = x.to(t)
+    w = torch.eye(n, k, device="cuda").to(t)
+    y = torch.empty(rows, n, dtype=t, device="cuda")
+    ctx.linear(T.Matrix(x), T.Matrix(w), T.Matrix(y), workspace=space(ctx.linear_workspace(rows, k, n)))
+    ctx.sync()
+    m = min(k, n)
+    assert torch.equal(y[:, :m], x[:, :m]) and not y[:, m:].any()
+
+
 def test_small_gradients_of_float16_through_scales(T, ctx):
     """scales of 2^-20 and gradients of 2^-10: their product alone would be lost in float16"""
     t = torch.float16
