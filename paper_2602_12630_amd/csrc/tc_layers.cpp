@@ -81,49 +81,79 @@ uint32_t slope_groups(uint32_t rows, uint32_t cols) {
 }
 /* How a product of np x nq results over nr is laid out: the tile, and into how many parts r is split so that there are workgroups for
  * the whole chip. */
-struct ProductPlan {
+struct Layout {
     uint32_t np, nq, side, splits, r_split;
     uint64_t ldp;
-    uint64_t tiles(uint32_t sp, uint32_t sq) const { return (uint64_t)((np + sp - 1) / sp) * ((nq + sq - 1) / sq); }
+    uint64_t tiles(uint32_t s) const { return (uint64_t)((np + s - 1) / s) * ((nq + s - 1) / s); }
     size_t part_bytes() const { return splits > 1 ? (size_t)splits * nq * ldp * 4 : 0; }
-    /* with the 16-bit copy of an int8 operand, which the kernel of the largest tiles wants */
-    size_t bytes(uint32_t nr) const { return part_bytes() + (side == 256 ? up((size_t)np * nr * 2, 256) : 0); }
 };
 /* Chosen by what the layouts cost, in microseconds, measured over products of 10^9 to 10^12 multiply-adds: so much for a step of 64 r
  * with one, two .. workgroups on every compute unit (as many as LDS holds), one for a round of workgroups to start and finish in, and
  * for a split the writing and reading of its parts at 6 GB a millisecond and one more launch.  Within 10 % of the best layout
  * wherever both were timed: 8192 x 4096 -> 11008: 256 x 256 641 us, 128 x 128 672, 64 x 64 992; 487 x 11008 -> 4096: 128 x 128 in four parts
  * 52 us, whole 114, 256 x 256 in eight parts 61; 64 x 4096 -> 4096: 64 x 64 in eight parts 15 us, whole 33, 128 x 128 whole 42. */
-ProductPlan product_plan(uint32_t np, uint32_t nq, uint32_t nr) {
-    struct Layout {
+Layout product_layout(uint32_t np, uint32_t nq, uint32_t nr, double* least) {
+    struct Rate {
         uint32_t side, deepest;
         double step[5];
     };
-    static const Layout layouts[3] = {{256, 1, {1.7}}, {128, 2, {0.75, 0.97}}, {64, 5, {0.48, 0.5, 0.62, 0.75, 0.9}}};
+    static const Rate rates[3] = {{256, 1, {1.7}}, {128, 2, {0.75, 0.97}}, {64, 5, {0.48, 0.5, 0.62, 0.75, 0.9}}};
     static const uint32_t parts[] = {1, 2, 3, 4, 6, 8, 12, 16};
-    ProductPlan best = {np, nq, 64, 1, nr, up(np, 8)};
-    if (!nq || !nr) return best;                     /* no rows: nothing is launched */
-    double least = 1e300;
-    for (const Layout& l : layouts)
+    Layout best = {np, nq, 64, 1, nr, up(np, 8)};
+    *least = 1e300;
+    if (!np || !nq || !nr) return best;              /* no rows: nothing is launched */
+    for (const Rate& l : rates)
         for (uint32_t splits : parts) {
-            ProductPlan p = {np, nq, l.side, 1, nr, up(np, 8)};
+            Layout p = {np, nq, l.side, 1, nr, up(np, 8)};
             if (splits > 1) {
                 p.r_split = (uint32_t)up((nr + splits - 1) / splits, 64);
                 p.splits = (nr + p.r_split - 1) / p.r_split;
                 if (p.splits != splits || p.r_split < 256) break;
             }
-            const double groups = (double)p.tiles(l.side, l.side) * splits, steps = (p.r_split + 63) / 64;
+            const double groups = (double)p.tiles(l.side) * splits, steps = (p.r_split + 63) / 64;
             const uint32_t deep = (uint32_t)std::min<double>(l.deepest, std::ceil(groups / 256));
             double rounds = groups / (256.0 * deep);
-            if (rounds < 3) rounds = std::ceil(rounds);
+            if (rounds < 3 || l.deepest == 1) rounds = std::ceil(rounds);
             double cost = rounds * (steps * l.step[deep - 1] + 1);
             if (splits > 1) cost += 4 + (double)p.part_bytes() * 2 / 6e6;
-            if (cost < least) {
-                least = cost;
+            if (cost < *least) {
+                *least = cost;
                 best = p;
             }
         }
     return best;
+}
+/* The largest tiles are one to a compute unit, and a last round with few of them leaves most of the chip idle: where it pays, whole
+ * rounds of them take the product up to `cut` of p (or q), and a launch of another layout takes the rest.  8192 x 4096 -> 11008 with gelu: 1376 tiles in
+ * 732 us, 1280 of them and 384 of 128 x 128 in 682. */
+struct ProductPlan {
+    Layout whole, first, rest;
+    uint32_t cut;                    /* 0: the product is done as a whole */
+    bool cut_p;
+    /* the parts of split sums; behind them, the 16-bit copy of an int8 operand, which the kernel of the largest tiles wants */
+    size_t part_bytes() const { return std::max(whole.part_bytes(), cut ? rest.part_bytes() : 0); }
+    size_t bytes(uint32_t nr) const { return part_bytes() + (whole.side == 256 ? up((size_t)whole.np * nr * 2, 256) : 0); }
+};
+ProductPlan product_plan(uint32_t np, uint32_t nq, uint32_t nr) {
+    ProductPlan p = {};
+    double least;
+    p.whole = product_layout(np, nq, nr, &least);
+    if (p.whole.side != 256 || p.whole.splits > 1) return p;
+    const uint32_t tp = (np + 255) / 256, tq = (nq + 255) / 256, rounds = (uint32_t)(p.whole.tiles(256) / 256);
+    for (int on_p = 0; on_p < 2; ++on_p) {
+        const uint64_t lines = (uint64_t)rounds * 256 / (on_p ? tq : tp);            /* whole lines of tiles in whole rounds */
+        if (lines == 0 || lines >= (on_p ? tp : tq)) continue;
+        const uint32_t cut = (uint32_t)lines * 256;
+        double a, b;
+        const Layout first = product_layout(on_p ? cut : np, on_p ? nq : cut, nr, &a), rest = product_layout(on_p ? np - cut : np, on_p ? nq : nq - cut, nr, &b);
+        if (first.side != 256 || first.splits > 1 || a + b + 4 >= least) continue;
+        least = a + b + 4;
+        p.first = first;
+        p.rest = rest;
+        p.cut = cut;
+        p.cut_p = on_p;
+    }
+    return p;
 }
 /* workspace of the linear gradients: where each part lies */
 struct BackPlan {
@@ -237,59 +267,88 @@ int allow_lds(tc_ctx* ctx, const void* kernel, size_t bytes, std::atomic<uint64_
     said.fetch_or(bit, std::memory_order_relaxed);
     return TC_OK;
 }
+/* one product by one layout; loose: 0, or how its operands have to be read (see Feed) */
+template <class T, bool P_ALONG, bool P_EIGHT, bool Q_ALONG, bool FORWARD>
+int multiply_by(tc_ctx* ctx, ProductArgs a, const Layout& l, int loose, float* part) {
+    a.r_split = l.r_split;
+    if (l.splits > 1) {
+        a.part = part;
+        a.ldp = l.ldp;
+    }
+    const uint64_t tiles128 = l.tiles(128) * l.splits, tiles64 = l.tiles(64) * l.splits;
+    const size_t lds256 = 5 * 512 * 32 * 2, lds128 = 2 * 256 * 64 * 2, lds64 = 2 * 128 * 64 * 2;
+    if (loose == 2) TRY(launch_product(ctx, product_paired<T, P_ALONG, P_EIGHT, Q_ALONG, FORWARD, 2, 64, 64, 2, 2>, a, tiles64, 256, lds64));
+    else if (loose && l.side > 64) TRY(launch_product(ctx, product_paired<T, P_ALONG, P_EIGHT, Q_ALONG, FORWARD, 1, 128, 128, 2, 2>, a, tiles128, 256, lds128));
+    else if (loose) TRY(launch_product(ctx, product_paired<T, P_ALONG, P_EIGHT, Q_ALONG, FORWARD, 1, 64, 64, 2, 2>, a, tiles64, 256, lds64));
+    else if (l.side == 256) {
+        if constexpr (P_EIGHT) REFUSE(TC_ERR_STATE, "internal: int8 operand that was not widened");
+        else {
+            auto* kernel = product_deep<T, P_ALONG, Q_ALONG, FORWARD, 256, 256, 2, 4>;
+            static std::atomic<uint64_t> said{0};
+            TRY(allow_lds(ctx, (const void*)kernel, lds256, said));
+            TRY(launch_product(ctx, kernel, a, l.tiles(256) * l.splits, 512, lds256));
+        }
+    } else if (l.side == 128) TRY(launch_product(ctx, product_paired<T, P_ALONG, P_EIGHT, Q_ALONG, FORWARD, 0, 128, 128, 2, 2>, a, tiles128, 256, lds128));
+    else TRY(launch_product(ctx, product_paired<T, P_ALONG, P_EIGHT, Q_ALONG, FORWARD, 0, 64, 64, 2, 2>, a, tiles64, 256, lds64));
+    if (l.splits > 1) {
+        const uint64_t pieces8 = (uint64_t)((a.np + 7) / 8) * a.nq;
+        hipLaunchKernelGGL((join_parts<T, FORWARD>), dim3((uint32_t)((pieces8 + 255) / 256)), dim3(256), 0, ctx_stream(ctx), a, l.splits);
+        int e = (int)hipGetLastError();
+        if (e) return ctx_fail_hip(ctx, e, "launch of join_parts");
+    }
+    return TC_OK;
+}
+/* 16-bit operands in whole pieces, in the one or two launches of the plan */
+template <class T, bool P_ALONG, bool Q_ALONG, bool FORWARD>
+int multiply_planned(tc_ctx* ctx, const ProductArgs& a, const ProductPlan& plan, float* part) {
+    if (!plan.cut) return multiply_by<T, P_ALONG, false, Q_ALONG, FORWARD>(ctx, a, plan.whole, 0, part);
+    const uint64_t cut = plan.cut;
+    ProductArgs first = a, rest = a;
+    auto behind = [](const void* p, uint64_t elements) { return p ? (const char*)p + elements * sizeof(T) : nullptr; };
+    if (plan.cut_p) {
+        first.np = plan.cut;
+        rest.np = a.np - plan.cut;
+        rest.p.d = behind(a.p.d, P_ALONG ? cut * a.p.ld : cut);
+        rest.out = (void*)behind(a.out, cut);
+        rest.p_scale = a.p_scale ? a.p_scale + cut : nullptr;
+        rest.bias = behind(a.bias, cut);
+        rest.residual = behind(a.residual, cut);
+        rest.z = (void*)behind(a.z, cut);
+    } else {
+        first.nq = plan.cut;
+        rest.nq = a.nq - plan.cut;
+        rest.q.d = behind(a.q.d, Q_ALONG ? cut * a.q.ld : cut);
+        rest.out = (void*)behind(a.out, cut * a.ldo);
+        rest.residual = behind(a.residual, cut * a.ldres);
+        rest.z = (void*)behind(a.z, cut * a.ldz);
+    }
+    TRY((multiply_by<T, P_ALONG, false, Q_ALONG, FORWARD>(ctx, first, plan.first, 0, part)));
+    return multiply_by<T, P_ALONG, false, Q_ALONG, FORWARD>(ctx, rest, plan.rest, 0, part);
+}
 template <class T, bool P_ALONG, bool P_EIGHT, bool Q_ALONG, bool FORWARD>
 int multiply(tc_ctx* ctx, ProductArgs a, float* part) {
-    const bool pieces = in_pieces(a.p, P_ALONG ? a.nr : a.np, P_EIGHT) && in_pieces(a.q, Q_ALONG ? a.nr : a.nq, false);
     /* Up to sixteen rows: a pass over the weights alone, 1 x 4096 -> 4096 in 6.9 us against 10.5 by tiles.  Every workgroup reads all of x, though:
      * beyond eight rows, 16-bit weights that are past the caches' help go by tiles (16 x 4096 -> 11008: 18.4 us against 25.0). */
-    const bool few = a.nq <= 8 || (a.nq <= 16 && (P_EIGHT || (uint64_t)a.np * a.nr <= 1u << 25));
     if constexpr (FORWARD) {
+        const bool few = a.nq <= 8 || (a.nq <= 16 && (P_EIGHT || (uint64_t)a.np * a.nr <= 1u << 25));
         constexpr int waves = P_EIGHT ? 16 : 8;
         if (few && in_pieces(a.p, a.nr, P_EIGHT, true) && in_pieces(a.q, a.nr, false, true))
             return launch_product(ctx, product_thin<T, P_EIGHT, waves>, a, (a.np + 15) / 16, waves * 64, 0);
     }
     const ProductPlan plan = product_plan(a.np, a.nq, a.nr);
-    a.r_split = plan.r_split;
-    if (plan.splits > 1) {
-        a.part = part;
-        a.ldp = plan.ldp;
-    }
-    const uint64_t tiles = plan.tiles(plan.side, plan.side) * plan.splits, tiles128 = plan.tiles(128, 128) * plan.splits;
-    const size_t lds128 = 2 * 256 * 64 * 2, lds64 = 2 * 128 * 64 * 2;
-    if (!pieces) {
-        const uint64_t tiles64 = plan.tiles(64, 64) * plan.splits;
-        if ((P_ALONG ? a.nr : a.np) < 8 || (Q_ALONG ? a.nr : a.nq) < 8)
-            TRY(launch_product(ctx, product_paired<T, P_ALONG, P_EIGHT, Q_ALONG, FORWARD, 2, 64, 64, 2, 2>, a, tiles64, 256, lds64));
-        else if (plan.side > 64)
-            TRY(launch_product(ctx, product_paired<T, P_ALONG, P_EIGHT, Q_ALONG, FORWARD, 1, 128, 128, 2, 2>, a, tiles128, 256, lds128));
-        else
-            TRY(launch_product(ctx, product_paired<T, P_ALONG, P_EIGHT, Q_ALONG, FORWARD, 1, 64, 64, 2, 2>, a, tiles64, 256, lds64));
-    } else if (plan.side == 256) {
-        if (P_EIGHT) {
-            const uint32_t lines = P_ALONG ? a.np : a.nr, cols = P_ALONG ? a.nr : a.np;
-            T* wide = (T*)((uint8_t*)part + plan.part_bytes());
-            hipLaunchKernelGGL(widen_rows<T>, dim3((cols + 2047) / 2048, std::min<uint32_t>(lines, 65535)), dim3(256), 0, ctx_stream(ctx), a.p, wide, cols, lines, cols);
-            int e = (int)hipGetLastError();
-            if (e) return ctx_fail_hip(ctx, e, "launch of widen_rows");
-            a.p = Operand{wide, cols};
-        }
-        const size_t lds = 5 * 512 * 32 * 2;
-        auto* kernel = product_deep<T, P_ALONG, Q_ALONG, FORWARD, 256, 256, 2, 4>;
-        static std::atomic<uint64_t> said{0};
-        TRY(allow_lds(ctx, (const void*)kernel, lds, said));
-        TRY(launch_product(ctx, kernel, a, tiles, 512, lds));
-    } else if (plan.side == 128) {
-        TRY(launch_product(ctx, product_paired<T, P_ALONG, P_EIGHT, Q_ALONG, FORWARD, 0, 128, 128, 2, 2>, a, tiles, 256, lds128));
-    } else {
-        TRY(launch_product(ctx, product_paired<T, P_ALONG, P_EIGHT, Q_ALONG, FORWARD, 0, 64, 64, 2, 2>, a, tiles, 256, lds64));
-    }
-    if (plan.splits > 1) {
-        const uint64_t pieces8 = (uint64_t)((a.np + 7) / 8) * a.nq;
-        hipLaunchKernelGGL((join_parts<T, FORWARD>), dim3((uint32_t)((pieces8 + 255) / 256)), dim3(256), 0, ctx_stream(ctx), a, plan.splits);
+    const uint32_t along_p = P_ALONG ? a.nr : a.np, along_q = Q_ALONG ? a.nr : a.nq;
+    if (!in_pieces(a.p, along_p, P_EIGHT) || !in_pieces(a.q, along_q, false))
+        return multiply_by<T, P_ALONG, P_EIGHT, Q_ALONG, FORWARD>(ctx, a, plan.whole, along_p < 8 || along_q < 8 ? 2 : 1, part);
+    if constexpr (P_EIGHT) {
+        if (plan.whole.side != 256) return multiply_by<T, P_ALONG, true, Q_ALONG, FORWARD>(ctx, a, plan.whole, 0, part);
+        const uint32_t lines = P_ALONG ? a.np : a.nr, cols = along_p;
+        T* wide = (T*)((uint8_t*)part + plan.part_bytes());
+        hipLaunchKernelGGL(widen_rows<T>, dim3((cols + 2047) / 2048, std::min<uint32_t>(lines, 65535)), dim3(256), 0, ctx_stream(ctx), a.p, wide, cols, lines, cols);
         int e = (int)hipGetLastError();
-        if (e) return ctx_fail_hip(ctx, e, "launch of join_parts");
+        if (e) return ctx_fail_hip(ctx, e, "launch of widen_rows");
+        a.p = Operand{wide, cols};
     }
-    return TC_OK;
+    return multiply_planned<T, P_ALONG, Q_ALONG, FORWARD>(ctx, a, plan, part);
 }
 
 template <class T>

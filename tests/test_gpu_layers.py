@@ -626,7 +626,9 @@ def test_offsets_past_32_bits(T, ctx):
 
 
 # every layout of a product and every way of splitting it: sizes at which each of them is the cheapest for one of the three products
-LARGE = [(8200, 136, 8456), (8200, 8456, 136), (136, 8456, 8200), (487, 4104, 4104), (4104, 1040, 1040), (300, 4104, 520), (200, 200, 4104), (1100, 2056, 520)]
+LARGE = [(8200, 136, 8456), (8200, 8456, 136), (136, 8456, 8200), (487, 4104, 4104), (4104, 1040, 1040), (300, 4104, 520), (200, 200, 4104), (1100, 2056, 520),
+         # whole rounds of the largest tiles and the rest by others: cut along either axis, in each of the three products
+         (8456, 520, 8200), (10248, 520, 8200), (8456, 8200, 520), (10248, 8200, 520), (520, 8200, 8456), (520, 8200, 10248)]
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
@@ -638,16 +640,16 @@ def test_products_of_every_layout(T, ctx, dtype, eight, rows, k, n):
     x, mw, w64 = linear_inputs(T, t, rows, k, n, eight, seed, (0, 0))
     work = space(ctx.linear_workspace(rows, k, n))
     work.fill_(0xFF)
-    bias = rand((n,), seed + 2, t)
+    bias, residual = rand((n,), seed + 2, t), rand((rows, n), seed + 3, t)
     ybuf, y = empty(rows, n, t)
     z = torch.empty(rows, n, dtype=t, device="cuda")
-    ctx.linear(T.Matrix(x), mw, T.Matrix(y), bias=bias, activation=T.TC_ACT_GELU, z=T.Matrix(z), workspace=work)
+    ctx.linear(T.Matrix(x), mw, T.Matrix(y), bias=bias, activation=T.TC_ACT_GELU, residual=T.Matrix(residual), z=T.Matrix(z), workspace=work)
     ctx.sync()
     z64 = x.double() @ w64.t() + bias.double()
     ez = ref.product_error(x.double().abs() @ w64.abs().t() + bias.double().abs(), k + 2)
     ok(z, z64, ez + ref.u(t) * (z64.abs() + ez) + ref.tiny(t))
-    y64 = ref.activate(z64, "gelu")
-    ey = 1.13 * ez + ref.activation_error(z64, "gelu")
+    y64 = ref.activate(z64, "gelu") + residual.double()
+    ey = 1.13 * ez + ref.activation_error(z64, "gelu") + ref.E * y64.abs()
     ok(y, y64, ey + ref.u(t) * (y64.abs() + ey) + ref.tiny(t))
     assert untouched(ybuf, rows, n)
     del z64, ez, y64, ey
