@@ -411,6 +411,17 @@ int run_linear_backward(tc_ctx* ctx, const tc_matrix* dy, const tc_matrix* x, co
         int e = (int)hipGetLastError();
         if (e) return ctx_fail_hip(ctx, e, "launch of scale_peak");
     }
+    /* (whatever else the call asks for, so that a sum does not depend on that) */
+    const bool direct = act == TC_ACT_NONE && dbias && rows <= 2048;
+    if (direct) {
+        const T* d = (const T*)dy->d_data;
+        const dim3 grid((out + 63) / 64), block(1024);
+        if (out < 8) hipLaunchKernelGGL((bias_sums<T, true>), grid, block, 0, ctx_stream(ctx), d, dy->ld, rows, out, dbias);
+        else hipLaunchKernelGGL((bias_sums<T, false>), grid, block, 0, ctx_stream(ctx), d, dy->ld, rows, out, dbias);
+        int e = (int)hipGetLastError();
+        if (e) return ctx_fail_hip(ctx, e, "launch of bias_sums");
+        dbias = nullptr;
+    }
     if (act != TC_ACT_NONE || by_x || by_w || dbias) {
         SlopeArgs s = {};
         s.dy = dy->d_data;
