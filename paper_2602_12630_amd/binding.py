@@ -288,13 +288,11 @@ def _ptr(x):
     return ctypes.c_void_p(int(x))
 
 
-def _nbytes(x):
-    return 0 if x is None else x.numel() * x.element_size()
-
-
 class Matrix:
     """A view of a 2-D torch tensor (float16, bfloat16 or int8, stride 1 along the rows) for the layer operators; `scale`: for
-    int8, a float32 tensor with one entry for each row.  It keeps the tensors alive and may be used for any number of calls."""
+    int8, a float32 tensor with one entry for each row.  It keeps the tensors alive and may be used for any number of calls.
+    The calls are asynchronous on the context's stream: where tensors were made on another stream, that one waits for this (and
+    the other way round), and record_stream tells torch's allocator, as for any work on a second stream."""
 
     _DTYPES = {"torch.float16": TC_F16, "torch.bfloat16": TC_BF16, "torch.int8": TC_I8}
 
@@ -317,6 +315,10 @@ class Matrix:
         self.view = tc_matrix(tensor.data_ptr() or None, scale.data_ptr() or None if scale is not None else None, rows, cols, ld,
                               self._DTYPES[str(tensor.dtype)])
         self._as_parameter_ = ctypes.addressof(self.view)
+        self.place, self.form = tensor.get_device(), (rows, cols, tensor.dtype)
+
+
+_BARE = (0, 0, False)  # the form of a tc_matrix by reference: nothing that vectors could be held against
 
 
 class Srs:
@@ -426,6 +428,7 @@ class Context:
             raise TcError(rc, "tc_ctx_create failed (is a GPU visible?)")
         self.handle = h
         self._vk = {}
+        self._place = int(device) if lib is None else None     # (a host build has the CPU's memory)
 
     def _check(self, rc):
         if rc != TC_OK:
@@ -511,30 +514,69 @@ class Context:
 
     # -- layer operators -----------------------------------------------------------------------
     # dy, x, w, y, z, residual, dx, dz, dw, src and dst are Matrix objects; gamma, beta, bias, mean, rstd, dgamma, dbeta, dbias are
-    # contiguous tensors (16-bit parameters of the activations' type, float32 statistics and sums).
+    # contiguous tensors (16-bit parameters of the activations' type, float32 statistics and sums), all on the context's GPU.
+    def _here(self, *matrices):
+        place = self._place
+        if place is not None:
+            for m in matrices:
+                if m is not None and m.place != place:
+                    raise ValueError("a matrix that is not on the context's GPU")
+
+    def _vector(self, x, n, dtype):
+        """address of n contiguous entries of `dtype` (None: float32, False: any)"""
+        if x is None or isinstance(x, int):
+            return x
+        if x.numel() < n or not x.is_contiguous() or not (x.dtype is dtype or dtype is False or dtype is None and str(x.dtype) == "torch.float32"):
+            raise ValueError("a vector of %s, %d entries: %s needed, %d side by side" % (x.dtype, x.numel(), dtype or "torch.float32", n))
+        if self._place is not None and x.get_device() != self._place:
+            raise ValueError("a vector that is not on the context's GPU")
+        return x.data_ptr()
+
+    def _room(self, x):
+        if x is None:
+            return None, 0
+        if self._place is not None and x.get_device() != self._place or not x.is_contiguous():
+            raise ValueError("a workspace is a contiguous tensor on the context's GPU")
+        return x.data_ptr(), x.numel() * x.element_size()
+
     def checkpoint_encode(self, src, dst):
         """dst (int8 rows, scales) = the 8-bit form of src's rows"""
+        if self._place is not None and not src.place == dst.place == self._place:
+            self._here(src, dst)
         self._check(self.lib.tc_checkpoint_encode(self.handle, src, dst))
 
     def checkpoint_decode(self, src, dst):
+        if self._place is not None and not src.place == dst.place == self._place:
+            self._here(src, dst)
         self._check(self.lib.tc_checkpoint_decode(self.handle, src, dst))
 
     def norm(self, kind, x, gamma, beta, eps, y, mean=None, rstd=None):
-        self._check(self.lib.tc_norm(self.handle, kind, x, _ptr(gamma), _ptr(beta), eps, y, _ptr(mean), _ptr(rstd)))
+        if self._place is not None and not x.place == y.place == self._place:
+            self._here(x, y)
+        rows, cols, t = getattr(y, "form", _BARE)
+        self._check(self.lib.tc_norm(self.handle, kind, x, self._vector(gamma, cols, t), self._vector(beta, cols, t), eps, y,
+                                     self._vector(mean, rows, None), self._vector(rstd, rows, None)))
 
     def norm_backward(self, kind, dy, x, gamma, mean, rstd, dx, dgamma, dbeta, workspace):
         """workspace: a uint8 tensor of norm_backward_workspace(rows, cols) bytes"""
-        self._check(self.lib.tc_norm_backward(self.handle, kind, dy, x, _ptr(gamma), _ptr(mean), _ptr(rstd), dx, _ptr(dgamma),
-                                              _ptr(dbeta), _ptr(workspace), _nbytes(workspace)))
+        self._here(dy, x, dx)
+        rows, cols, t = getattr(dy, "form", _BARE)
+        self._check(self.lib.tc_norm_backward(self.handle, kind, dy, x, self._vector(gamma, cols, t), self._vector(mean, rows, None),
+                                              self._vector(rstd, rows, None), dx, self._vector(dgamma, cols, None), self._vector(dbeta, cols, None),
+                                              *self._room(workspace)))
 
     def linear(self, x, w, y, bias=None, activation=TC_ACT_NONE, residual=None, z=None, workspace=None):
         """workspace: a uint8 tensor of linear_workspace(rows, in, out) bytes"""
-        self._check(self.lib.tc_linear(self.handle, x, w, _ptr(bias), activation, residual, y, z, _ptr(workspace), _nbytes(workspace)))
+        self._here(x, w, y, residual, z)
+        _, out, t = getattr(y, "form", _BARE)
+        self._check(self.lib.tc_linear(self.handle, x, w, self._vector(bias, out, t), activation, residual, y, z, *self._room(workspace)))
 
     def linear_backward(self, dy, x, w, activation=TC_ACT_NONE, z=None, dz=None, dx=None, dw=None, dbias=None, workspace=None):
         """workspace: a uint8 tensor of linear_backward_workspace(rows, in, out) bytes"""
-        self._check(self.lib.tc_linear_backward(self.handle, dy, x, w, activation, z, dz, dx, dw, _ptr(dbias), _ptr(workspace),
-                                                _nbytes(workspace)))
+        self._here(dy, x, w, z, dz, dx, dw)
+        _, out, _ = getattr(dy, "form", _BARE)
+        self._check(self.lib.tc_linear_backward(self.handle, dy, x, w, activation, z, dz, dx, dw, self._vector(dbias, out, None),
+                                                *self._room(workspace)))
 
     def _workspace(self, call, *sizes):
         out = ctypes.c_size_t()

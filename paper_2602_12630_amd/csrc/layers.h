@@ -374,7 +374,7 @@ __global__ __launch_bounds__(256) void checkpoint_decode(const RowArgs a) {
 
 /* ---- norms --------------------------------------------------------------------------------------------
  * A row is read once and stays in registers: its mean, then the mean square about it (no difference of large sums), then y.
- * Short calls are launches (one row of 4096: 2.3 us in the kernel, 4.4 a call); 487 x 4096 4.3 us. */
+ * Short calls are launches (one row of 4096: 2.3 us in the kernel, 4.6 a call); 487 x 4096 4.3 us. */
 struct NormArgs {
     const void* x;
     const float* scale;              /* x is int8 where this is set */
@@ -503,7 +503,7 @@ __global__ __launch_bounds__(LANES) void norm_backward(const NormBackArgs a) {
         }
     const float per = 1.0f / (float)a.cols;
     const uint64_t step = (uint64_t)gridDim.x * SETS;
-    /* A row is kept as it was read and unpacked twice, for the sums and for dx: three rows' raw bits take fewer registers than one row's values (values kept across the barrier spilled: 16384 x 4096 in 175 us).
+    /* A row is kept as it was read and unpacked twice, for the sums and for dx: three rows' raw bits take fewer registers than one row's values (values kept across the barrier spilled: 16384 x 4096 in 179 us).
      * Where a lane has more than one chunk of a row there is no room for the next ones. */
     constexpr bool AHEAD = NCH == 1;
     typedef typename std::conditional<EIGHT, RawQ<TH, SHORT>, Raw<T, TH, SHORT>>::type RawX;

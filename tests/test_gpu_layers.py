@@ -692,3 +692,65 @@ def test_more_rows_than_a_launch_has_workgroups(T, ctx):
     x64 = x.double()
     want, _, rstd = ref.norm(x64, None, None, 1e-5, False)
     ok(y, want, ref.norm_bound(x64, None, None, want, rstd, t, False))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_rows_of_the_greatest_length(T, ctx, dtype):
+    most = 1 << 20
+    test_checkpoints(T, ctx, dtype, 2, most, (0, 0))
+    for rows, k, n in [(3, most, 16), (3, 16, most), (16, most - 1, 5), (17, 5, most - 1)]:
+        for w8 in (False, True):
+            test_linear(T, ctx, dtype, w8, rows, k, n, (0, 0))
+        test_linear_gradients(T, ctx, dtype, "none", False, False, False, rows, k, n, (0, 0))
+        test_linear_gradients(T, ctx, dtype, "gelu", True, True, True, rows, k, n, (0, 0))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("pad", [(8, 8), (16, 0), (1, 2)])
+@pytest.mark.parametrize("rows,k,n", [(1, 64, 96), (3, 7, 5), (5, 8, 9), (37, 72, 40), (65, 200, 264), (130, 1027, 513), (300, 4104, 520), (1100, 2056, 520)])
+def test_what_lies_between_the_rows_does_not_matter(T, ctx, dtype, rows, k, n, pad):
+    """the same bytes from buffers whose other columns hold sevens, NaNs and infinities"""
+    t = ref.DT[dtype]
+    x, w, dy, z = rand((rows, k), 1, t), rand((n, k), 2, t, k ** -0.5), rand((rows, n), 3, t), rand((rows, n), 4, t)
+    x8, w8, z8 = rows8(x), rows8(w), rows8(z)
+    work = space(max(ctx.linear_workspace(rows, k, n), ctx.linear_backward_workspace(rows, k, n), ctx.norm_backward_workspace(rows, k)))
+    seen = None
+    for between, between8 in ((7, 7), (float("nan"), -128), (float("inf"), 127)):
+        M = lambda m: T.Matrix(strided(m, *pad, sentinel=between)[1])  # noqa: E731
+        M8 = lambda m: T.Matrix(strided(m[0], *pad, sentinel=between8)[1], m[1])  # noqa: E731
+        e = lambda *s, dt=t: torch.empty(*s, dtype=dt, device="cuda")  # noqa: E731
+        got = []
+        for mx, mw, mz in ((M(x), M(w), M(z)), (M8(x8), M8(w8), M8(z8))):
+            mean, rstd, h, dh, dg, db = e(rows, dt=torch.float32), e(rows, dt=torch.float32), e(rows, k), e(rows, k), e(k, dt=torch.float32), e(k, dt=torch.float32)
+            ctx.norm(0, mx, None, None, 1e-5, T.Matrix(h), mean, rstd)
+            ctx.norm_backward(0, M(x), mx, None, mean, rstd, T.Matrix(dh), dg, db, work)
+            y, dz, dx, dw, dbias = e(rows, n), e(rows, n), e(rows, k), e(n, k), e(n, dt=torch.float32)
+            ctx.linear(M(x), mw, T.Matrix(y), residual=M(dy), workspace=work)
+            ctx.linear_backward(M(dy), mx, mw, 2, mz, T.Matrix(dz), T.Matrix(dx), T.Matrix(dw), dbias, work)
+            bare, dw2 = e(rows, k), e(n, k)
+            ctx.linear_backward(M(dy), mx, mw, dx=T.Matrix(bare), dw=T.Matrix(dw2), workspace=work)
+            q, s, back = e(rows, k, dt=torch.int8), e(rows, dt=torch.float32), e(rows, k)
+            ctx.checkpoint_encode(M(x), T.Matrix(q, s))
+            ctx.checkpoint_decode(M8(x8), T.Matrix(back))
+            ctx.sync()
+            got += [mean, rstd, h, dh, dg, db, y, dz, dx, dw, dbias, bare, dw2, q, s, back]
+        assert all(bool(torch.isfinite(g.float()).all()) for g in got)
+        assert seen is None or [i for i, (p, q) in enumerate(zip(seen, got)) if not torch.equal(p, q)] == []
+        seen = got
+
+
+def test_tensors_that_are_elsewhere_are_refused(T, ctx):
+    t = torch.float16
+    x, far = torch.zeros(4, 8, dtype=t, device="cuda"), torch.zeros(4, 8, dtype=t)
+    m, bad = T.Matrix(x), T.Matrix(far)
+    square, v = T.Matrix(torch.zeros(8, 8, dtype=t, device="cuda")), torch.zeros(8)
+    for call in (lambda: ctx.norm(0, bad, None, None, 1e-5, m), lambda: ctx.norm(0, m, None, None, 1e-5, bad),
+                 lambda: ctx.norm(0, m, v.to(t), None, 1e-5, m), lambda: ctx.norm(0, m, None, None, 1e-5, m, v, None),
+                 lambda: ctx.checkpoint_encode(bad, m), lambda: ctx.checkpoint_decode(m, bad),
+                 lambda: ctx.linear(bad, square, m), lambda: ctx.linear(m, square, m, residual=bad), lambda: ctx.linear(m, square, m, bias=v.to(t)),
+                 lambda: ctx.linear(m, square, m, workspace=torch.zeros(1 << 16, dtype=torch.uint8)),
+                 lambda: ctx.linear_backward(m, None, square, dx=bad, workspace=space(1 << 20)),
+                 lambda: ctx.linear_backward(m, None, square, dbias=v, workspace=space(1 << 20)),
+                 lambda: ctx.norm_backward(1, m, m, None, None, v, m, None, None, None)):
+        with pytest.raises(ValueError):
+            call()

@@ -290,3 +290,23 @@ def test_norm_and_linear_on_the_host(emu, dtype, eight):
     for got, w64 in ((dz, d), (dx, d @ vw), (dw, d.t() @ vx)):
         assert ref.worst(got, w64, (ref.u(t) + ref.E) * w64.abs() + ref.tiny(t) + 1e-12) <= 1
     assert ref.worst(db, d.sum(0), 2 * ref.E * d.sum(0).abs() + 1e-12) <= 1
+
+
+def test_vectors_of_torch_are_checked(emu):
+    """too short, of another type, with gaps"""
+    m, w = mat(4, 8), mat(8, 8)
+    h, f = torch.zeros(8, dtype=torch.float16), torch.zeros(8)
+    big = ws(1 << 20)
+    emu.norm(0, m, h, h, 1e-5, m, f[:4], f[:4])
+    emu.linear_backward(m, None, w, dx=mat(4, 8), dbias=f, workspace=big)
+    for bad in (h[:7], f, h.bfloat16(), torch.zeros(16, dtype=torch.float16)[::2]):
+        for call in (lambda: emu.norm(0, m, bad, None, 1e-5, m), lambda: emu.norm(0, m, None, bad, 1e-5, m),
+                     lambda: emu.norm_backward(0, m, m, bad, f, f, m, None, None, None), lambda: emu.linear(m, w, m, bias=bad)):
+            with pytest.raises(ValueError):
+                call()
+    for bad in (f[:3], h, f.double(), torch.zeros(16)[::2]):
+        for call in (lambda: emu.norm(0, m, None, None, 1e-5, m, bad, None), lambda: emu.norm(0, m, None, None, 1e-5, m, None, bad),
+                     lambda: emu.norm_backward(0, m, m, None, f, f, m, bad, None, big), lambda: emu.norm_backward(0, m, m, None, f, bad, m, None, None, big),
+                     lambda: emu.linear_backward(m, None, w, dx=m, dbias=bad, workspace=big)):
+            with pytest.raises(ValueError):
+                call()
