@@ -241,20 +241,25 @@ __device__ __forceinline__ void load8q(const int8_t* p, float scale, int t, int 
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = scale * r.get(j);
 }
-/* eight values to entries k .. of a row of n */
+/* eight values to entries k .. of a row of n; `past`: past the caches */
 template <class T>
-__device__ __forceinline__ void put8(T* row, uint32_t k, uint32_t n, const float* v) {
+__device__ __forceinline__ void put8(T* row, uint32_t k, uint32_t n, const float* v, bool past = false) {
+    typedef typename Vec<T>::v8 anywhere __attribute__((aligned(2)));
     typename Vec<T>::v8 x;
 #pragma unroll
     for (int j = 0; j < 8; ++j) x[j] = (T)v[j];
-    if (k + 8 <= n) __builtin_memcpy(row + k, &x, 16);
-    else
+    if (k + 8 <= n) {
+        if (past) {
+            asm volatile("");            /* (else the compiler makes one plain store of the two) */
+            __builtin_nontemporal_store(x, (anywhere*)(row + k));
+        } else *(anywhere*)(row + k) = x;
+    } else
 #pragma unroll
         for (int j = 0; j < 7; ++j)
             if (k + j < n) row[k + j] = x[j];
 }
 template <class T, int TH>
-__device__ __forceinline__ void store8(T* p, int t, int c, uint32_t cols, const float* v) { put8<T>(p, row_col<TH>(t, c), cols, v); }
+__device__ __forceinline__ void store8(T* p, int t, int c, uint32_t cols, const float* v, bool past = false) { put8<T>(p, row_col<TH>(t, c), cols, v, past); }
 
 /* ---- 8-bit checkpoints ------------------------------------------------------------------------------- */
 struct RowArgs {
@@ -263,6 +268,7 @@ struct RowArgs {
     float* scale;
     uint64_t ld_src, ld_dst;
     uint32_t rows, cols;
+    bool past;                       /* the 16-bit output goes past the caches */
 };
 /* The row is scaled by a power of two so that amax, the largest finite magnitude, lies in [1, 2): nothing overflows or gets lost (but entries
  * below 2^-126 of amax, whose q is 0 either way).  x and amax have at most 11 significant bits, so t = 127 x has 18 and is exact in
@@ -368,7 +374,7 @@ __global__ __launch_bounds__(256) void checkpoint_decode(const RowArgs a) {
     for (uint64_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
         float v[8];
         load8q<256, SHORT>((const int8_t*)a.src + row * a.ld_src, a.scale[row], threadIdx.x, blockIdx.x, a.cols, v);
-        store8<T, 256>((T*)a.dst + row * a.ld_dst, threadIdx.x, blockIdx.x, a.cols, v);
+        store8<T, 256>((T*)a.dst + row * a.ld_dst, threadIdx.x, blockIdx.x, a.cols, v, a.past);
     }
 }
 
@@ -482,6 +488,7 @@ struct NormBackArgs {
     uint64_t lddy, ldx, lddx;
     uint32_t rows, cols;
     int centred;
+    bool past;                       /* dx goes past the caches */
 };
 template <class T, bool EIGHT, int TH, int NCH, int LANES, bool SHORT = false>
 __global__ __launch_bounds__(LANES) void norm_backward(const NormBackArgs a) {
@@ -557,7 +564,7 @@ __global__ __launch_bounds__(LANES) void norm_backward(const NormBackArgs a) {
                 const float h = (now.x[c].get(j) * now.scale - now.mean) * now.rstd, d = now.dy[c].get(j), g = a.gamma ? d * gamma[c].get(j) : d;
                 v[j] = now.rstd * (g - mg - h * mgx);
             }
-            store8<T, TH>((T*)a.dx + row * a.lddx, t, c, cols, v);
+            store8<T, TH>((T*)a.dx + row * a.lddx, t, c, cols, v, a.past);
         }
     };
     /* every lane of the workgroup makes the same rounds; the cells go round by three, so one barrier a round is enough */
@@ -655,6 +662,7 @@ struct ProductArgs {
     uint64_t ldz;
     const float* factor;             /* gradients: everything times this number; null: 1 */
     int act;
+    bool past;                       /* out and z go past the caches */
     float* part;                     /* [split][nq][ldp] unfinished sums, where r is split; null: the whole of r in one go */
     uint64_t ldp;
     uint32_t r_split;                /* r of one split */
@@ -739,7 +747,7 @@ struct Finish {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[i] += bias[i];
             }
-            if (a.z) put8<T>((T*)a.z + q * a.ldz, p, a.np, v);
+            if (a.z) put8<T>((T*)a.z + q * a.ldz, p, a.np, v, a.past);
             if (a.act != TC_ACT_NONE) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[i] = activate(v[i], a.act);
@@ -752,7 +760,7 @@ struct Finish {
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] *= scale[0];
         }
-        put8<T>((T*)a.out + q * a.ldo, p, a.np, v);
+        put8<T>((T*)a.out + q * a.ldo, p, a.np, v, a.past);
     }
 };
 /* A wave's NP x NQ blocks of sixteen by sixteen, through a piece of LDS of its own (NP * 16 + 4 floats for each of sixteen q): a lane of

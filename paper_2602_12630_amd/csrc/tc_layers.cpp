@@ -186,6 +186,11 @@ using namespace tc::layers;
         if (e_) return ctx_fail_hip(ctx, e_, "launch of " #kernel);                         \
     } while (0)
 
+/* Whether a 16-bit output is written past the caches.  The last-level cache holds 256 MB: from half of that on, an output would drive out what the call
+ * and the next one read, and little of it is left when it is read itself.  256 MB decoded: 57 us against 70, with a norm that reads them 162
+ * against 166; the gradient of a norm of 128 MB 74 against 85, with a checkpoint of it 128 against 125; 8192 x 4096 -> 11008 672 against 686.  Smaller outputs
+ * are better read from the cache: 64 MB decoded and normalised 46 us past it, 44 through it.  (A norm's own output gains nothing.) */
+bool past_caches(const tc_matrix* m) { return (uint64_t)m->rows * m->cols * 2 >= 128u << 20; }
 /* workgroups for `sets` sets of rows; the kernels go round until all are done */
 uint32_t row_grid(uint64_t sets) { return (uint32_t)std::min<uint64_t>(sets, 1u << 20); }
 template <class T>
@@ -353,12 +358,12 @@ int multiply(tc_ctx* ctx, ProductArgs a, float* part) {
 
 template <class T>
 int run_encode(tc_ctx* ctx, const tc_matrix* src, const tc_matrix* dst) {
-    const RowArgs a{src->d_data, dst->d_data, dst->d_scale, src->ld, dst->ld, src->rows, src->cols};
+    const RowArgs a{src->d_data, dst->d_data, dst->d_scale, src->ld, dst->ld, src->rows, src->cols, false};
     return encode_rows<T>(ctx, a);
 }
 template <class T>
 int run_decode(tc_ctx* ctx, const tc_matrix* src, const tc_matrix* dst) {
-    const RowArgs a{src->d_data, dst->d_data, src->d_scale, src->ld, dst->ld, src->rows, src->cols};
+    const RowArgs a{src->d_data, dst->d_data, src->d_scale, src->ld, dst->ld, src->rows, src->cols, past_caches(dst)};
     const dim3 grid((a.cols + 2047) / 2048, std::min<uint32_t>(a.rows, 65535));
     if (a.cols < 8) LAUNCH((checkpoint_decode<T, true>), grid, 256, 0, a);
     else LAUNCH((checkpoint_decode<T, false>), grid, 256, 0, a);
@@ -375,7 +380,7 @@ int run_norm_backward(tc_ctx* ctx, int kind, const tc_matrix* dy, const tc_matri
     const uint32_t groups = norm_back_groups(dy->rows, dy->cols);
     float* part = dgamma || dbeta ? (float*)ws : nullptr;
     const NormBackArgs a{dy->d_data, x->d_data, x->dtype == TC_I8 ? x->d_scale : nullptr, gamma, mean, rstd, dx ? dx->d_data : nullptr, part,
-                         dy->ld, x->ld, dx ? dx->ld : 0, dy->rows, dy->cols, kind == TC_NORM_LAYER};
+                         dy->ld, x->ld, dx ? dx->ld : 0, dy->rows, dy->cols, kind == TC_NORM_LAYER, past_caches(dy)};
     TRY((a.scale ? norm_back_rows<T, true>(ctx, a, groups) : norm_back_rows<T, false>(ctx, a, groups)));
     return part ? sum_columns(ctx, part, 2 * (uint64_t)dy->cols, groups, dy->cols, dgamma, dbeta) : TC_OK;
 }
@@ -395,6 +400,7 @@ int run_linear(tc_ctx* ctx, const tc_matrix* x, const tc_matrix* w, const void* 
     if (residual) { a.residual = residual->d_data; a.ldres = residual->ld; }
     if (z) { a.z = z->d_data; a.ldz = z->ld; }
     a.act = act;
+    a.past = past_caches(y);
     return a.p_scale ? multiply<T, true, true, true, true>(ctx, a, (float*)ws) : multiply<T, true, false, true, true>(ctx, a, (float*)ws);
 }
 template <class T>
@@ -460,6 +466,7 @@ int run_linear_backward(tc_ctx* ctx, const tc_matrix* dy, const tc_matrix* x, co
         a.out = dx->d_data;
         a.ldo = dx->ld;
         a.factor = by_w && m ? m + 2 : nullptr;
+        a.past = past_caches(dx);
         TRY((by_w ? multiply<T, false, true, true, false>(ctx, a, parts) : multiply<T, false, false, true, false>(ctx, a, parts)));
     }
     if (dw) {
@@ -472,6 +479,7 @@ int run_linear_backward(tc_ctx* ctx, const tc_matrix* dy, const tc_matrix* x, co
         a.out = dw->d_data;
         a.ldo = dw->ld;
         a.factor = by_x ? m : nullptr;
+        a.past = past_caches(dw);
         TRY((by_x ? multiply<T, false, true, false, false>(ctx, a, parts) : multiply<T, false, false, false, false>(ctx, a, parts)));
     }
     return TC_OK;
