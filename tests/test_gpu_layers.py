@@ -754,3 +754,14 @@ def test_tensors_that_are_elsewhere_are_refused(T, ctx):
                  lambda: ctx.norm_backward(1, m, m, None, None, v, m, None, None, None)):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("width", [4096, 4101])
+def test_outputs_larger_than_the_caches_keep(T, ctx, dtype, width):
+    """outputs of 128 MB and more, which are written past the caches, with rows at any alignment"""
+    test_checkpoints(T, ctx, dtype, 16400, width, (0, 0))
+    test_norm_and_its_gradient(T, ctx, dtype, "layer", 16400, width, (1, 2))
+    test_linear(T, ctx, dtype, True, 16400, 40, width, (1, 2))
+    test_linear_gradients(T, ctx, dtype, "none", True, False, False, 16400, width, 40, (1, 2))
+    test_linear_gradients(T, ctx, dtype, "gelu", False, True, True, 40, 16400, width, (0, 0))
