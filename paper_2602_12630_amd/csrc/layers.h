@@ -477,7 +477,9 @@ __global__ __launch_bounds__(TH < 256 ? 256 : TH) void norm_forward(const NormAr
 /* The gradient: a workgroup of LANES lanes takes LANES / TH rows at a time and every gridDim-th such set; a lane keeps the sums of dy xh and dy
  * for its columns over all of them, so that gamma's and beta's gradients cost one partial row per workgroup and no second
  * pass over the activations.  The next two sets' loads are under way while this one's two sums are formed, at one barrier a set.  The row sets of a workgroup are added in order through LDS; column_sums adds the workgroups.
- * Bound by memory: 16384 x 4096 from int8 rows in 82 us, 335 MB, 4.1 GB a millisecond (copies reach 5.2). */
+ * Partial sums leave in pieces of 32 bytes: entry by entry 29 x 11008 took 19 us instead of 11, 512 x 4096 16 instead of 13.
+ * Bound by memory: 16384 x 4096 from int8 rows in 78 us, 335 MB, 4.3 GB a millisecond (copies reach 5.2).  Rows beyond 8192 (16384) entries keep some 50 (480) bytes
+ * a lane in scratch memory, 29 x 32768 takes 41 us. */
 struct NormBackArgs {
     const void *dy, *x;
     const float* scale;
@@ -597,16 +599,25 @@ __global__ __launch_bounds__(LANES) void norm_backward(const NormBackArgs a) {
             if (SETS > 1) __syncthreads();
             if (set != s) continue;
 #pragma unroll
-            for (int c = 0; c < NCH; ++c)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const uint32_t k = row_col<TH>(t, c) + j;
-                    if (k >= a.cols) continue;
-                    float v = which ? db[c][j] : dg[c][j];
-                    if (s) v += lds[k];
-                    if (s + 1 < SETS) lds[k] = v;
-                    else part[k] = v;
+            for (int c = 0; c < NCH; ++c) {
+                const uint32_t k = row_col<TH>(t, c);
+                if (k >= a.cols) continue;
+                const float* mine = which ? db[c] : dg[c];
+                f4 v[2] = {{mine[0], mine[1], mine[2], mine[3]}, {mine[4], mine[5], mine[6], mine[7]}};
+                f4* sum = (f4*)(lds + k);            /* (LDS has room for whole pieces of eight) */
+                if (s) {
+                    v[0] += sum[0];
+                    v[1] += sum[1];
                 }
+                if (s + 1 < SETS) {
+                    sum[0] = v[0];
+                    sum[1] = v[1];
+                } else if (k + 8 <= a.cols) __builtin_memcpy(part + k, v, 32);
+                else
+#pragma unroll
+                    for (int j = 0; j < 7; ++j)
+                        if (k + j < a.cols) part[k + j] = v[j / 4][j % 4];
+            }
         }
     }
 }

@@ -220,7 +220,7 @@ int norm_rows(tc_ctx* ctx, const NormArgs& a) {
 template <class T, bool EIGHT>
 int norm_back_rows(tc_ctx* ctx, const NormBackArgs& a, uint32_t groups) {
     const uint32_t c = a.cols, sets = norm_back_sets(a.rows, c);
-    const size_t lds = sets > 1 ? (size_t)c * 4 : 0;
+    const size_t lds = sets > 1 ? up(c, 8) * 4 : 0;
     if (a.rows < 1024) {                             /* few rows: smaller workgroups, so that they go to more compute units */
         if (c < 8) LAUNCH((norm_backward<T, EIGHT, 64, 1, 256, true>), groups, 256, lds, a);
         else if (c <= 512) LAUNCH((norm_backward<T, EIGHT, 64, 1, 256>), groups, 256, lds, a);
