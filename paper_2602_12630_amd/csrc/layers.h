@@ -672,6 +672,7 @@ struct ProductArgs {
     void* z;
     uint64_t ldz;
     const float* factor;             /* gradients: everything times this number; null: 1 */
+    const uint16_t* powers;          /* gradients in float16, int8 p: a power of two for each r, in float16, that its whole numbers are multiplied by */
     int act;
     bool past;                       /* out and z go past the caches */
     float* part;                     /* [split][nq][ldp] unfinished sums, where r is split; null: the whole of r in one go */
@@ -851,7 +852,7 @@ template <class T, bool ALONG, bool EIGHT, int LOOSE, int SIDE, int TH, int BK>
 struct Feed {
     typedef Tile<T, ALONG, SIDE, BK> tile;
     static constexpr int N = SIDE * BK / 8 / TH, PIECES = ALONG ? BK / 8 : SIDE / 8, SIZE = EIGHT ? 1 : 2;
-    static constexpr bool HELD = EIGHT || LOOSE != 0;
+    static constexpr bool HELD = EIGHT || LOOSE != 0, POWERS = EIGHT && !ALONG && std::is_same<T, _Float16>::value;
     static constexpr uint32_t NOWHERE = 0x80000000u;
     typedef typename std::conditional<EIGHT, uint2, uint4>::type Piece;
     typedef Piece Held[HELD ? N : 1];
@@ -860,6 +861,8 @@ struct Feed {
     uint64_t step, ld;
     uint32_t nr, line_bytes, left;   /* left: of the operand's axis across the sum, from this tile on */
     uint32_t held_rest;              /* of the sum, from the tile in `held` on */
+    const uint16_t* powers;
+    uint32_t held_power[POWERS ? N : 1];
     __device__ static __forceinline__ int line_of(int n) { return n / PIECES; }
     __device__ static __forceinline__ int piece_of(int n) {
         const int line = n / PIECES, slot = n % PIECES;
@@ -871,8 +874,9 @@ struct Feed {
         return end > has ? end - has : 0;
     }
     /* r from `r0` on, `nr_` of them */
-    __device__ __forceinline__ void init(const Operand& o, uint64_t side0, uint32_t sides, uint32_t r0, uint32_t nr_, int t) {
+    __device__ __forceinline__ void init(const Operand& o, uint64_t side0, uint32_t sides, uint32_t r0, uint32_t nr_, int t, const uint16_t* powers_ = nullptr) {
         nr = nr_;
+        if constexpr (POWERS) powers = powers_ + r0;
         ld = o.ld;
         left = sides - (uint32_t)side0;
         line_bytes = (uint32_t)(o.ld * SIZE);
@@ -890,6 +894,11 @@ struct Feed {
     __device__ __forceinline__ void issue(T* lds, Held& held, uint32_t k, int t) {
         const uint32_t rest = __builtin_amdgcn_readfirstlane(nr > k * BK ? nr - k * BK : 0);      /* a saturating difference, which is a vector instruction */
         const char* at = base + (rest ? k * step : 0);
+        if constexpr (POWERS) {          /* a line past the last one gets 0 */
+            const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)(powers + (rest ? k * BK : 0)), 0, (rest < BK ? rest : BK) * 2, 0x00020000);
+#pragma unroll
+            for (int i = 0; i < N; ++i) held_power[i] = __builtin_amdgcn_raw_buffer_load_b16(r, line_of(i * TH + t) * 2, 0, 0);
+        }
         if constexpr (LOOSE == 1) {
             held_rest = rest;
             if (!rest) return;
@@ -949,7 +958,8 @@ struct Feed {
                         for (uint32_t& x : w) x = 0;
                     else if (b) to_front(w, 8 - b);
                 }
-                if constexpr (EIGHT) *to = widen<T>(w[0], w[1]);
+                if constexpr (POWERS) *to = widen<T>(w[0], w[1]) * __builtin_bit_cast(T, (uint16_t)held_power[i]);
+                else if constexpr (EIGHT) *to = widen<T>(w[0], w[1]);
                 else *to = __builtin_bit_cast(typename Vec<T>::v8, make_uint4(w[0], w[1], w[2], w[3]));
             }
         }
@@ -982,7 +992,7 @@ __device__ __forceinline__ void tile_of(uint32_t b, uint32_t tiles_p, uint32_t t
     const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6), wp = w % WP, wq = w / WP;         \
     FP fp;                                                                                                                  \
     FQ fq;                                                                                                                  \
-    fp.init(a.p, p0, a.np, r0, nr, t);                                                                                      \
+    fp.init(a.p, p0, a.np, r0, nr, t, a.powers);                                                                            \
     fq.init(a.q, q0, a.nq, r0, nr, t);                                                                                      \
     f4 acc[NP][NQ] = {};
 #define TC_WAIT_AND_MEET(n) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(n) : "memory")
@@ -1083,14 +1093,17 @@ __global__ __launch_bounds__(WP * WQ * 64) __attribute__((amdgpu_waves_per_eu(WP
 #undef TC_PRODUCT_PROLOGUE
 #undef TC_PRODUCT_EPILOGUE
 
-/* int8 rows -> the same whole numbers in T, side by side with a stride of ldo: 256 lanes take 2048 entries of a row */
+/* int8 rows -> the same whole numbers in T, times a power of two for each row where `powers` has them, side by side with a stride of ldo: 256 lanes
+ * take 2048 entries of a row */
 template <class T>
-__global__ __launch_bounds__(256) void widen_rows(const Operand o, T* out, uint64_t ldo, uint32_t rows, uint32_t cols) {
+__global__ __launch_bounds__(256) void widen_rows(const Operand o, const uint16_t* powers, T* out, uint64_t ldo, uint32_t rows, uint32_t cols) {
     const uint32_t col = (blockIdx.x * 256 + threadIdx.x) * 8;
     if (col >= cols) return;
     for (uint64_t row = blockIdx.y; row < rows; row += gridDim.y) {
         const uint2 q = *(const uint2*)((const int8_t*)o.d + row * o.ld + col);
-        *(typename Vec<T>::v8*)(out + row * ldo + col) = widen<T>(q.x, q.y);
+        typename Vec<T>::v8 v = widen<T>(q.x, q.y);
+        if (std::is_same<T, _Float16>::value && powers) v *= __builtin_bit_cast(T, powers[row]);
+        *(typename Vec<T>::v8*)(out + row * ldo + col) = v;
     }
 }
 
@@ -1192,22 +1205,27 @@ __global__ __launch_bounds__(WAVES * 64) void product_thin(const ProductArgs a) 
 
 /* ---- the gradient before the activation ------------------------------------------------------------------
  * dz = dy act'(z), and its sums over the rows.  int8 operands of the products that follow have a scale for each of the
- * rows that those products sum over; it is put into their other operand here, from the unrounded value: by_x = dz s_x[row] / m_x for dw,
- * by_w = dz s_w[column] / m_w for dx.  So whole numbers enter the matrix instruction exactly and one rounding of the
- * gradient is all there is.  m is the power of two above the largest scale: it keeps float16 in its range and is put back, exactly, after the product (bfloat16 has
- * float32's range and takes m = 1). */
+ * rows that those products sum over; it is put into their other operand here, from the unrounded value: by_x = dz s_x[row] for dw,
+ * by_w = dz s_w[column] for dx.  So whole numbers enter the matrix instruction exactly and one rounding of the gradient to its type is all there is.
+ * bfloat16 has float32's range and takes the scale as it is.  float16 would lose rows whose scale is small beside the largest, so a scale is split into a number of
+ * [1/2, 1), which goes to the gradient and cannot overflow, and a power of two, which goes to the whole numbers as they are widened: relative to the largest
+ * scale's, which becomes 2^8, down to 2^-24 every q 2^k is a float16.  (Scales more than 2^32 below the largest leave the rest with the gradient.)  One row of 512 with an entry of
+ * 5000 among others of N(0, 1), gradients of 1e-4: dw of the other columns is 3.3e-4 of its size off; with one power of two for all rows it was 0.41. */
 struct SlopeArgs {
     const void *dy, *z;
     const float* z_scale;            /* z is int8 where this is set */
     void *dz, *by_x, *by_w;
     const float *x_scale, *w_scale;
-    const float* m;                  /* m_x, 1 / m_x, m_w, 1 / m_w; null: ones */
+    const float* m;                  /* float16: what scale_peak wrote */
+    uint16_t *powers_x, *powers_w;   /* float16: the powers of two of x's and w's rows */
     float* part;                     /* [gridDim.y][cols] */
     uint64_t lddy, ldz, lddz;        /* by_x, by_w: cols side by side, padded to ld_by */
     uint64_t ld_by;
     uint32_t rows, cols;
     int act;
 };
+/* for the largest magnitude f 2^e of x's scales, f in [1/2, 1): m[0] = 2^(e - 8), which their product is multiplied by, m[1] = e; of w's: m[2], m[3].  e is
+ * held above -110, so that m[0] is in the normal range. */
 __global__ __launch_bounds__(1024) void scale_peak(const float* x, uint32_t nx, const float* w, uint32_t nw, float* m) {
     __shared__ float cells[16];
     const float* s = blockIdx.x ? w : x;
@@ -1218,9 +1236,16 @@ __global__ __launch_bounds__(1024) void scale_peak(const float* x, uint32_t nx, 
     v = group_max<1024>(v, cells, threadIdx.x);
     if (threadIdx.x) return;
     int e = v > 0.0f ? ilogbf(v) + 1 : 0;
-    e = e < -120 ? -120 : e > 120 ? 120 : e;
-    m[2 * blockIdx.x] = ldexpf(1.0f, e);
-    m[2 * blockIdx.x + 1] = ldexpf(1.0f, -e);
+    e = e < -110 ? -110 : e;
+    m[2 * blockIdx.x] = ldexpf(1.0f, e - 8);
+    m[2 * blockIdx.x + 1] = (float)e;
+}
+/* the scale s = f 2^e beside the largest one's 2^top: its power of two, 2^(8 + e - top) as a float16, and what is left for the gradient (0, infinities and NaNs: they themselves) */
+__device__ __forceinline__ float split_scale(float s, int top, uint16_t& power) {
+    const float f = __builtin_amdgcn_frexp_mantf(s);
+    const int below = __builtin_amdgcn_frexp_expf(s) - top, held = below < -32 ? -32 : below > 0 ? 0 : below, k = held + 8;
+    power = (uint16_t)(k < -14 ? 1 << (k + 24) : (k + 15) << 10);
+    return below < -32 ? ldexpf(f, below + 32) : f;
 }
 /* A wave takes 512 columns (eight to a lane), the four waves of a workgroup every fourth of its rows. */
 template <class T, bool SHORT>
@@ -1229,10 +1254,16 @@ __global__ __launch_bounds__(256) void slopes(const SlopeArgs a) {
     const int w = threadIdx.x >> 6, t = threadIdx.x & 63, strip = blockIdx.x;
     const uint32_t k = row_col<64>(t, strip);
     float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0}, ws[8];
-    const float mx = a.by_x && a.m ? a.m[1] : 1.0f, mw = a.by_w && a.m ? a.m[3] : 1.0f;
+    const int top_x = a.by_x && a.m ? (int)a.m[1] : 0, top_w = a.by_w && a.m ? (int)a.m[3] : 0;
     if (a.by_w)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) ws[j] = k + j < a.cols ? a.w_scale[k + j] * mw : 0.0f;
+        for (int j = 0; j < 8; ++j) {
+            ws[j] = k + j < a.cols ? a.w_scale[k + j] : 0.0f;
+            if (!a.m) continue;
+            uint16_t power;
+            ws[j] = split_scale(ws[j], top_w, power);
+            if (blockIdx.y == 0 && w == 0 && k + j < a.cols) a.powers_w[k + j] = power;
+        }
     for (uint64_t row = (uint64_t)blockIdx.y * 4 + w; row < a.rows; row += (uint64_t)gridDim.y * 4) {
         float v[8], z[8];
         load8<T, 64, SHORT>((const T*)a.dy + row * a.lddy, t, strip, a.cols, v);
@@ -1246,7 +1277,12 @@ __global__ __launch_bounds__(256) void slopes(const SlopeArgs a) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) sum[j] += v[j];
         if (a.by_x) {
-            const float f = a.x_scale[row] * mx;
+            float f = a.x_scale[row];
+            if (a.m) {
+                uint16_t power;
+                f = split_scale(f, top_x, power);
+                if (strip == 0 && t == 0) a.powers_x[row] = power;
+            }
 #pragma unroll
             for (int j = 0; j < 8; ++j) z[j] = v[j] * f;
             put8<T>((T*)a.by_x + row * a.ld_by, k, a.cols, z);

@@ -157,7 +157,7 @@ ProductPlan product_plan(uint32_t np, uint32_t nq, uint32_t nr) {
 }
 /* workspace of the linear gradients: where each part lies */
 struct BackPlan {
-    size_t by_x, by_w, part, m, split, bytes;
+    size_t by_x, by_w, part, m, powers_x, powers_w, split, bytes;
     uint64_t ld_by;
 };
 /* in = 0: neither dx nor dw is wanted */
@@ -169,7 +169,9 @@ BackPlan back_plan(uint32_t rows, uint32_t in, uint32_t out) {
     b.by_w = scaled;
     b.part = 2 * scaled;
     b.m = b.part + up((size_t)slope_groups(rows, out) * out * 4, 256);
-    b.split = b.m + 256;
+    b.powers_x = b.m + 256;
+    b.powers_w = b.powers_x + up((size_t)rows * 2, 256);
+    b.split = b.powers_w + up((size_t)out * 2, 256);
     b.bytes = b.split + (in ? std::max(product_plan(in, rows, out).bytes(out), product_plan(in, out, rows).bytes(rows)) : 0);
     return b;
 }
@@ -348,7 +350,7 @@ int multiply(tc_ctx* ctx, ProductArgs a, float* part) {
         if (plan.whole.side != 256) return multiply_by<T, P_ALONG, true, Q_ALONG, FORWARD>(ctx, a, plan.whole, 0, part);
         const uint32_t lines = P_ALONG ? a.np : a.nr, cols = along_p;
         T* wide = (T*)((uint8_t*)part + plan.part_bytes());
-        hipLaunchKernelGGL(widen_rows<T>, dim3((cols + 2047) / 2048, std::min<uint32_t>(lines, 65535)), dim3(256), 0, ctx_stream(ctx), a.p, wide, cols, lines, cols);
+        hipLaunchKernelGGL(widen_rows<T>, dim3((cols + 2047) / 2048, std::min<uint32_t>(lines, 65535)), dim3(256), 0, ctx_stream(ctx), a.p, a.powers, wide, cols, lines, cols);
         int e = (int)hipGetLastError();
         if (e) return ctx_fail_hip(ctx, e, "launch of widen_rows");
         a.p = Operand{wide, cols};
@@ -409,7 +411,7 @@ int run_linear_backward(tc_ctx* ctx, const tc_matrix* dy, const tc_matrix* x, co
     const uint32_t rows = dy->rows, out = dy->cols;
     const BackPlan plan = back_plan(rows, dx ? dx->cols : dw ? dw->cols : 0, out);
     uint8_t* base = (uint8_t*)ws;
-    /* powers of two beside the scales, which bfloat16 can do without */
+    /* float16: the scales' powers of two apart from the rest of them (see slopes) */
     float *m = std::is_same<T, _Float16>::value ? (float*)(base + plan.m) : nullptr, *parts = (float*)(base + plan.split);
     const bool by_x = dw && x->dtype == TC_I8, by_w = dx && w->dtype == TC_I8;
     if (m && (by_x || by_w)) {
@@ -444,6 +446,8 @@ int run_linear_backward(tc_ctx* ctx, const tc_matrix* dy, const tc_matrix* x, co
         s.x_scale = by_x ? x->d_scale : nullptr;
         s.w_scale = by_w ? w->d_scale : nullptr;
         s.m = m;
+        s.powers_x = (uint16_t*)(base + plan.powers_x);
+        s.powers_w = (uint16_t*)(base + plan.powers_w);
         s.part = dbias ? (float*)(base + plan.part) : nullptr;
         s.ld_by = plan.ld_by;
         s.rows = rows;
@@ -466,6 +470,7 @@ int run_linear_backward(tc_ctx* ctx, const tc_matrix* dy, const tc_matrix* x, co
         a.out = dx->d_data;
         a.ldo = dx->ld;
         a.factor = by_w && m ? m + 2 : nullptr;
+        a.powers = by_w && m ? (const uint16_t*)(base + plan.powers_w) : nullptr;
         a.past = past_caches(dx);
         TRY((by_w ? multiply<T, false, true, true, false>(ctx, a, parts) : multiply<T, false, false, true, false>(ctx, a, parts)));
     }
@@ -479,6 +484,7 @@ int run_linear_backward(tc_ctx* ctx, const tc_matrix* dy, const tc_matrix* x, co
         a.out = dw->d_data;
         a.ldo = dw->ld;
         a.factor = by_x ? m : nullptr;
+        a.powers = by_x && m ? (const uint16_t*)(base + plan.powers_x) : nullptr;
         a.past = past_caches(dw);
         TRY((by_x ? multiply<T, false, true, false, false>(ctx, a, parts) : multiply<T, false, false, false, false>(ctx, a, parts)));
     }

@@ -765,3 +765,84 @@ def test_outputs_larger_than_the_caches_keep(T, ctx, dtype, width):
     test_linear(T, ctx, dtype, True, 16400, 40, width, (1, 2))
     test_linear_gradients(T, ctx, dtype, "none", True, False, False, 16400, width, 40, (1, 2))
     test_linear_gradients(T, ctx, dtype, "gelu", False, True, True, 40, 16400, width, (0, 0))
+
+
+def spread_inputs(t, rows, k, n, spread, size, quiet, act, seed):
+    """x and w as int8 rows of which some stand out by `spread` (one large entry, as a first token has), gradients of the given size, zero for those rows
+    and outputs where `quiet`"""
+    x, w, dy = rand((rows, k), seed, t), rand((n, k), seed + 1, t, k ** -0.5), rand((rows, n), seed + 2, t, size)
+    loud_x, loud_w = torch.arange(0, rows, 37, device="cuda"), torch.arange(0, n, 41, device="cuda")
+    x[loud_x, loud_x % k], w[loud_w, loud_w % k] = 3.0 * spread, 3.0 * k ** -0.5 * spread
+    if quiet:
+        dy[loud_x], dy[:, loud_w] = 0, 0
+    z = rand((rows, n), seed + 3, t) if act != "none" else None
+    return rows8(x), rows8(w), dy, z
+
+
+# a wave's worth, rows of fewer than eight entries and of no whole pieces, sums in several parts, and each kind of tile
+SPREAD = [(40, 64, 48), (9, 5, 7), (70, 65, 33), (300, 200, 520), (487, 1032, 1096), (520, 8200, 8456), (8456, 520, 8200)]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,k,n", SPREAD)
+@pytest.mark.parametrize("act,spread,size,quiet", [("none", 2.0 ** 4, 1e-2, False), ("none", 2.0 ** 9, 1e-3, True), ("gelu", 2.0 ** 12, 1e-3, False), ("none", 2.0 ** 14, 1e-4, True)])
+def test_gradients_through_scales_that_differ_widely(T, ctx, dtype, rows, k, n, act, spread, size, quiet):
+    """A row whose scale stands out costs the others nothing.  The gradient times what its scale has beside a power of two, a number from 1/2 to 1, is rounded to the
+    type: half a step of it, and below the normal range half the smallest step, which is at most a whole one in units of the gradient."""
+    t = ref.DT[dtype]
+    qx, qw, dy, z = spread_inputs(t, rows, k, n, spread, size, quiet, act, rows + k + n)
+    mz, mdz = (T.Matrix(z), T.Matrix(torch.empty_like(dy))) if z is not None else (None, None)
+    dx, dw = torch.empty(rows, k, dtype=t, device="cuda"), torch.empty(n, k, dtype=t, device="cuda")
+    work = space(ctx.linear_backward_workspace(rows, k, n))
+    work.fill_(0xFF)
+    ctx.linear_backward(T.Matrix(dy), T.Matrix(*qx), T.Matrix(*qw), ref.ACTS[act], mz, mdz, T.Matrix(dx), T.Matrix(dw), workspace=work)
+    ctx.sync()
+    x64, w64, d64 = ref.value(*qx), ref.value(*qw), dy.double()
+    e = torch.zeros_like(d64)
+    if z is not None:
+        s = ref.slope(z.double(), act)
+        e = d64.abs() * ref.slope_error(z.double(), act) + 2 * ref.E * (d64 * s).abs()
+        d64 = d64 * s
+    off = (ref.u(t) + 3 * ref.E) * (d64.abs() + e) + e + 2 * ref.tiny(t)
+    for got, left, right, terms in ((dx, (d64, off), w64, n), (dw, (d64.t(), off.t()), x64, rows)):
+        want = left[0] @ right
+        err = left[1] @ right.abs()
+        err = err + ref.product_error((left[0].abs() + left[1]) @ right.abs(), terms)
+        ok(got, want, err + ref.u(t) * (want.abs() + err) + ref.tiny(t))
+        if quiet:                                           # the rows that stand out add nothing: what the others give is as exact as ever
+            # (a rounding of the gradient and one of the result, each at most half a step; below the normal range a step of it against its size)
+            rel = (got.double() - want).norm() / want.norm()
+            assert rel < 2 * ref.u(t) + 4 * ref.tiny(t) / size + ref.tiny(t) * want.numel() ** 0.5 / want.norm(), rel
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,k,n", [(40, 64, 48), (70, 65, 33), (520, 8200, 8456)])
+def test_gradients_through_scales_of_every_kind(T, ctx, dtype, rows, k, n):
+    """scales of zero, below zero, below the normal range, and so far below the largest that their rows show only because its gradient is zero"""
+    t = ref.DT[dtype]
+    (qx, sx), (qw, sw) = rows8(rand((rows, k), 1, t)), rows8(rand((n, k), 2, t))
+    dy = rand((rows, n), 3, t)
+    top = torch.tensor([1.0, 0.0, -1.0, 2.0 ** -31, -2.0 ** -33, 2.0 ** -38, 1e-40, 2.0 ** -32], device="cuda")
+    sx = (2.0 ** 31 * top[torch.arange(rows, device="cuda") % 8]) * (sx / sx.max())
+    sw = (2.0 ** 28 * top[torch.arange(n, device="cuda") % 8]) * (sw / sw.max())
+    dy[sx.abs() > 2.0 ** 10], dy[:, sw.abs() > 2.0 ** 10] = 0, 0
+    dx, dw = torch.empty(rows, k, dtype=t, device="cuda"), torch.empty(n, k, dtype=t, device="cuda")
+    ctx.linear_backward(T.Matrix(dy), T.Matrix(qx, sx), T.Matrix(qw, sw), dx=T.Matrix(dx), dw=T.Matrix(dw), workspace=space(ctx.linear_backward_workspace(rows, k, n)))
+    ctx.sync()
+    d64, x64, w64 = dy.double(), ref.value(qx, sx), ref.value(qw, sw)
+    for got, left, right, scale, terms in ((dx, d64, w64, sw[None, :], n), (dw, d64.t(), x64, sx[None, :], rows)):
+        # beyond 2^32 below the largest a scale's rest is with the gradient, whose smallest step counts for that much more
+        size = scale.double().abs()
+        below = torch.where(size == 0, torch.ones_like(size), size.max() / size * 2.0 ** -31).clamp(min=1)
+        off = (ref.u(t) + 3 * ref.E) * left.abs() + 2 * ref.tiny(t) * below
+        want = left @ right
+        err = off @ right.abs()
+        err = err + ref.product_error((left.abs() + off) @ right.abs(), terms)
+        ok(got, want, err + ref.u(t) * (want.abs() + err) + ref.tiny(t))
+        assert got.any()
+    for bad in (float("nan"), float("inf")):                # not a number in, none out: in its own sum over the rows, which is every one of dw
+        sx[3] = bad
+        dy[3] = 1
+        ctx.linear_backward(T.Matrix(dy), T.Matrix(qx, sx), None, dw=T.Matrix(dw), workspace=space(ctx.linear_backward_workspace(rows, k, n)))
+        ctx.sync()
+        assert not torch.isfinite(dw).any()
