@@ -846,3 +846,27 @@ def test_gradients_through_scales_of_every_kind(T, ctx, dtype, rows, k, n):
         ctx.linear_backward(T.Matrix(dy), T.Matrix(qx, sx), None, dw=T.Matrix(dw), workspace=space(ctx.linear_backward_workspace(rows, k, n)))
         ctx.sync()
         assert not torch.isfinite(dw).any()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("act,least", [("gelu", 13.0), ("silu", 80.0)])
+def test_activations_far_below_zero_are_rounded_once(T, ctx, dtype, act, least):
+    """Every number of the type from -least to 0, against a bound relative to the result.  The exponential's argument has three roundings (two for silu), so it is
+    off by 1.5 z^2 (2 |z|) half steps of float32; 24 (8) more for the tail's fit, its terms, the reciprocal and the products."""
+    t = ref.DT[dtype]
+    z = torch.arange(0, 1 << 15, device="cuda").to(torch.int16).view(t)
+    z = -z[torch.isfinite(z) & (z <= least)]
+    n, zero = z.numel(), torch.zeros(1, 8, device="cuda", dtype=t)
+    y, dz = torch.empty(1, n, dtype=t, device="cuda"), torch.empty(1, n, dtype=t, device="cuda")
+    w = torch.zeros(n, 8, device="cuda", dtype=t)
+    ctx.linear(T.Matrix(zero), T.Matrix(w), T.Matrix(y), bias=z, activation=ref.ACTS[act], workspace=space(ctx.linear_workspace(1, 8, n)))
+    ctx.linear_backward(T.Matrix(torch.ones_like(y)), None, None, ref.ACTS[act], T.Matrix(z[None, :]), T.Matrix(dz), workspace=space(ctx.linear_backward_workspace(1, 8, n)))
+    ctx.sync()
+    v = z.double()
+    rel = ((1.5 * v * v + 24) if act == "gelu" else (2 * v.abs() + 8)) * ref.E
+    want = ref.activate(v, act)
+    ok(y[0], want, rel * want.abs() + ref.u(t) * (1 + rel) * want.abs() + ref.tiny(t))
+    # the slope is a sum of two terms with that error each
+    terms = ref.phi(v) + v.abs() * torch.exp(-0.5 * v * v) / (2.0 * torch.pi) ** 0.5 if act == "gelu" else torch.sigmoid(v) * (1 + v.abs())
+    want, e = ref.slope(v, act), rel * terms
+    ok(dz[0], want, e + ref.u(t) * (want.abs() + e) + ref.tiny(t))
