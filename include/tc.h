@@ -235,7 +235,8 @@ int tc_encode_batch_scaled(tc_ctx* ctx, int count, const void* const* d_src, con
  * that the gradients were taken from.
  *
  * All of them are asynchronous on the context's stream, allocate nothing, read nothing back and may be captured into a
- * graph; scratch memory is the caller's (the *_workspace calls say how much).  The same call on the same data gives the same bytes, every time: no
+ * graph; scratch memory is the caller's (the *_workspace calls say how much, for every type and choice of outputs).  A workspace that is large enough for
+ * some number of rows serves calls of fewer rows (of the same columns) too.  The same call on the same data gives the same bytes, every time: no
  * sum depends on the order in which workgroups run.  Sums, statistics and products are held in 32 bits; results are
  * rounded once to their type.  Outputs may not overlap inputs or one another, but for: y in the place of the residual
  * (tc_linear), y in the place of x (tc_norm), dx in the place of dy (tc_norm_backward), dz in the place of dy
@@ -289,6 +290,8 @@ int tc_norm_backward_workspace(uint32_t rows, uint32_t cols, size_t* bytes);
 #define TC_ACT_SILU 3
 int tc_linear(tc_ctx* ctx, const tc_matrix* x, const tc_matrix* w, const void* d_bias, int activation, const tc_matrix* residual,
               const tc_matrix* y, const tc_matrix* z, void* d_workspace, size_t workspace_bytes);
+/* What the fastest layout of the product takes, which is not always more for more rows (products of many rows need no parts of sums).  In a smaller workspace,
+ * or none, the call takes the best layout that fits, whose sums are formed in another order. */
 int tc_linear_workspace(uint32_t rows, uint32_t in, uint32_t out, size_t* bytes);
 /* Its gradients:  dz = dy act'(z),  dx = dz w,  dw = dz^T x,  dbias = sum over rows of dz (relu'(0) = 0; the residual's gradient is dy itself).
  * z and x: as the forward pass had them, in 16 bits or as checkpoints; w as there.  With an activation z and dz are needed; without one
@@ -297,6 +300,7 @@ int tc_linear_workspace(uint32_t rows, uint32_t in, uint32_t out, size_t* bytes)
 int tc_linear_backward(tc_ctx* ctx, const tc_matrix* dy, const tc_matrix* x, const tc_matrix* w, int activation, const tc_matrix* z,
                        const tc_matrix* dz, const tc_matrix* dx, const tc_matrix* dw, float* d_dbias, void* d_workspace,
                        size_t workspace_bytes);
+/* The same; less than that of as many rows with in = 1 is refused, since the gradients before the products need so much. */
 int tc_linear_backward_workspace(uint32_t rows, uint32_t in, uint32_t out, size_t* bytes);
 
 /* ---- Com (Def. 4.1, Com) -------------------------------------------------------- */

@@ -123,7 +123,7 @@ inline void norm_backward(int dtype, int kind, const tc_matrix* dy, const tc_mat
         if (dbeta) dbeta[c] = (float)db[c];
     }
 }
-inline void linear(int dtype, const tc_matrix* x, const tc_matrix* w, const void* bias, int act, const tc_matrix* residual, const tc_matrix* y, const tc_matrix* z, void*) {
+inline void linear(int dtype, const tc_matrix* x, const tc_matrix* w, const void* bias, int act, const tc_matrix* residual, const tc_matrix* y, const tc_matrix* z, void*, size_t) {
     for (size_t r = 0; r < x->rows; ++r)
         for (size_t o = 0; o < w->rows; ++o) {
             double v = bias ? load16(bias, o, dtype) : 0;
@@ -134,7 +134,7 @@ inline void linear(int dtype, const tc_matrix* x, const tc_matrix* w, const void
         }
 }
 inline void linear_backward(int, const tc_matrix* dy, const tc_matrix* x, const tc_matrix* w, int act, const tc_matrix* z, const tc_matrix* dz,
-                            const tc_matrix* dx, const tc_matrix* dw, float* dbias, void*) {
+                            const tc_matrix* dx, const tc_matrix* dw, float* dbias, void*, size_t) {
     const size_t rows = dy->rows, out = dy->cols, in = dx ? dx->cols : dw ? dw->cols : 0;
     std::vector<double> d(rows * out);
     for (size_t r = 0; r < rows; ++r)

@@ -74,6 +74,10 @@ uint32_t norm_back_groups(uint32_t rows, uint32_t cols) {
     const uint32_t sets = norm_back_sets(rows, cols);
     return std::min<uint32_t>(256, (rows + sets - 1) / sets);
 }
+/* and the most that this or a smaller number of rows has: below 1024 rows a workgroup has fewer of them */
+uint32_t norm_back_most_groups(uint32_t rows, uint32_t cols) {
+    return std::max(norm_back_groups(rows, cols), norm_back_groups(std::min<uint32_t>(rows, 1023), cols));
+}
 /* sets of rows over which the gradient before the activation is spread: about eight workgroups for each compute unit */
 uint32_t slope_groups(uint32_t rows, uint32_t cols) {
     const uint32_t strips = (cols + 511) / 512;
@@ -91,8 +95,9 @@ struct Layout {
  * with one, two .. workgroups on every compute unit (as many as LDS holds), one for a round of workgroups to start and finish in, and
  * for a split the writing and reading of its parts at 6 GB a millisecond and one more launch.  Within 10 % of the best layout
  * wherever both were timed: 8192 x 4096 -> 11008: 256 x 256 641 us, 128 x 128 672, 64 x 64 992; 487 x 11008 -> 4096: 128 x 128 in four parts
- * 52 us, whole 114, 256 x 256 in eight parts 61; 64 x 4096 -> 4096: 64 x 64 in eight parts 15 us, whole 33, 128 x 128 whole 42. */
-Layout product_layout(uint32_t np, uint32_t nq, uint32_t nr, double* least) {
+ * 52 us, whole 114, 256 x 256 in eight parts 61; 64 x 4096 -> 4096: 64 x 64 in eight parts 15 us, whole 33, 128 x 128 whole 42.  Layouts whose parts do
+ * not fit into `room` bytes and tiles larger than `largest` are left out. */
+Layout product_layout(uint32_t np, uint32_t nq, uint32_t nr, size_t room, uint32_t largest, double* least) {
     struct Rate {
         uint32_t side, deepest;
         double step[5];
@@ -102,7 +107,8 @@ Layout product_layout(uint32_t np, uint32_t nq, uint32_t nr, double* least) {
     Layout best = {np, nq, 64, 1, nr, up(np, 8)};
     *least = 1e300;
     if (!np || !nq || !nr) return best;              /* no rows: nothing is launched */
-    for (const Rate& l : rates)
+    for (const Rate& l : rates) {
+        if (l.side > largest) continue;
         for (uint32_t splits : parts) {
             Layout p = {np, nq, l.side, 1, nr, up(np, 8)};
             if (splits > 1) {
@@ -110,6 +116,7 @@ Layout product_layout(uint32_t np, uint32_t nq, uint32_t nr, double* least) {
                 p.splits = (nr + p.r_split - 1) / p.r_split;
                 if (p.splits != splits || p.r_split < 256) break;
             }
+            if (p.part_bytes() > room) break;
             const double groups = (double)p.tiles(l.side) * splits, steps = (p.r_split + 63) / 64;
             const uint32_t deep = (uint32_t)std::min<double>(l.deepest, std::ceil(groups / 256));
             double rounds = groups / (256.0 * deep);
@@ -121,6 +128,7 @@ Layout product_layout(uint32_t np, uint32_t nq, uint32_t nr, double* least) {
                 best = p;
             }
         }
+    }
     return best;
 }
 /* The largest tiles are one to a compute unit, and a last round with few of them leaves most of the chip idle: where it pays, whole
@@ -134,10 +142,10 @@ struct ProductPlan {
     size_t part_bytes() const { return std::max(whole.part_bytes(), cut ? rest.part_bytes() : 0); }
     size_t bytes(uint32_t nr) const { return part_bytes() + (whole.side == 256 ? up((size_t)whole.np * nr * 2, 256) : 0); }
 };
-ProductPlan product_plan(uint32_t np, uint32_t nq, uint32_t nr) {
+ProductPlan product_plan(uint32_t np, uint32_t nq, uint32_t nr, size_t room = SIZE_MAX, uint32_t largest = 256) {
     ProductPlan p = {};
     double least;
-    p.whole = product_layout(np, nq, nr, &least);
+    p.whole = product_layout(np, nq, nr, room, largest, &least);
     if (p.whole.side != 256 || p.whole.splits > 1) return p;
     const uint32_t tp = (np + 255) / 256, tq = (nq + 255) / 256, rounds = (uint32_t)(p.whole.tiles(256) / 256);
     for (int on_p = 0; on_p < 2; ++on_p) {
@@ -145,7 +153,8 @@ ProductPlan product_plan(uint32_t np, uint32_t nq, uint32_t nr) {
         if (lines == 0 || lines >= (on_p ? tp : tq)) continue;
         const uint32_t cut = (uint32_t)lines * 256;
         double a, b;
-        const Layout first = product_layout(on_p ? cut : np, on_p ? nq : cut, nr, &a), rest = product_layout(on_p ? np - cut : np, on_p ? nq : nq - cut, nr, &b);
+        const Layout first = product_layout(on_p ? cut : np, on_p ? nq : cut, nr, room, largest, &a),
+                     rest = product_layout(on_p ? np - cut : np, on_p ? nq : nq - cut, nr, room, largest, &b);
         if (first.side != 256 || first.splits > 1 || a + b + 4 >= least) continue;
         least = a + b + 4;
         p.first = first;
@@ -154,6 +163,14 @@ ProductPlan product_plan(uint32_t np, uint32_t nq, uint32_t nr) {
         p.cut_p = on_p;
     }
     return p;
+}
+/* The plan in a workspace of `room` bytes, which may be that of a larger call: sizes do not only grow with the rows (more rows may need no split).  Where there
+ * is less than the best plan wants, it is the best one that fits, at the least one without parts and with int8 operands through registers. */
+ProductPlan product_plan_in(uint32_t np, uint32_t nq, uint32_t nr, size_t room, bool eight) {
+    ProductPlan p = product_plan(np, nq, nr, room);
+    if (!eight || p.whole.side != 256 || p.bytes(nr) <= room) return p;
+    const size_t copy = p.bytes(nr) - p.part_bytes();
+    return room >= copy ? product_plan(np, nq, nr, room - copy) : product_plan(np, nq, nr, room, 128);
 }
 /* workspace of the linear gradients: where each part lies */
 struct BackPlan {
@@ -333,7 +350,7 @@ int multiply_planned(tc_ctx* ctx, const ProductArgs& a, const ProductPlan& plan,
     return multiply_by<T, P_ALONG, false, Q_ALONG, FORWARD>(ctx, rest, plan.rest, 0, part);
 }
 template <class T, bool P_ALONG, bool P_EIGHT, bool Q_ALONG, bool FORWARD>
-int multiply(tc_ctx* ctx, ProductArgs a, float* part) {
+int multiply(tc_ctx* ctx, ProductArgs a, float* part, size_t room) {
     /* Up to sixteen rows: a pass over the weights alone, 1 x 4096 -> 4096 in 6.9 us against 10.5 by tiles.  Every workgroup reads all of x, though:
      * beyond eight rows, 16-bit weights that are past the caches' help go by tiles (16 x 4096 -> 11008: 18.4 us against 25.0). */
     if constexpr (FORWARD) {
@@ -342,7 +359,7 @@ int multiply(tc_ctx* ctx, ProductArgs a, float* part) {
         if (few && in_pieces(a.p, a.nr, P_EIGHT, true) && in_pieces(a.q, a.nr, false, true))
             return launch_product(ctx, product_thin<T, P_EIGHT, waves>, a, (a.np + 15) / 16, waves * 64, 0);
     }
-    const ProductPlan plan = product_plan(a.np, a.nq, a.nr);
+    const ProductPlan plan = product_plan_in(a.np, a.nq, a.nr, part ? room : 0, P_EIGHT);
     const uint32_t along_p = P_ALONG ? a.nr : a.np, along_q = Q_ALONG ? a.nr : a.nq;
     if (!in_pieces(a.p, along_p, P_EIGHT) || !in_pieces(a.q, along_q, false))
         return multiply_by<T, P_ALONG, P_EIGHT, Q_ALONG, FORWARD>(ctx, a, plan.whole, along_p < 8 || along_q < 8 ? 2 : 1, part);
@@ -388,7 +405,7 @@ int run_norm_backward(tc_ctx* ctx, int kind, const tc_matrix* dy, const tc_matri
 }
 template <class T>
 int run_linear(tc_ctx* ctx, const tc_matrix* x, const tc_matrix* w, const void* bias, int act, const tc_matrix* residual, const tc_matrix* y, const tc_matrix* z,
-               void* ws) {
+               void* ws, size_t ws_bytes) {
     ProductArgs a = {};
     a.p = Operand{w->d_data, w->ld};
     a.q = Operand{x->d_data, x->ld};
@@ -403,13 +420,14 @@ int run_linear(tc_ctx* ctx, const tc_matrix* x, const tc_matrix* w, const void* 
     if (z) { a.z = z->d_data; a.ldz = z->ld; }
     a.act = act;
     a.past = past_caches(y);
-    return a.p_scale ? multiply<T, true, true, true, true>(ctx, a, (float*)ws) : multiply<T, true, false, true, true>(ctx, a, (float*)ws);
+    return a.p_scale ? multiply<T, true, true, true, true>(ctx, a, (float*)ws, ws_bytes) : multiply<T, true, false, true, true>(ctx, a, (float*)ws, ws_bytes);
 }
 template <class T>
 int run_linear_backward(tc_ctx* ctx, const tc_matrix* dy, const tc_matrix* x, const tc_matrix* w, int act, const tc_matrix* z, const tc_matrix* dz,
-                        const tc_matrix* dx, const tc_matrix* dw, float* dbias, void* ws) {
+                        const tc_matrix* dx, const tc_matrix* dw, float* dbias, void* ws, size_t ws_bytes) {
     const uint32_t rows = dy->rows, out = dy->cols;
     const BackPlan plan = back_plan(rows, dx ? dx->cols : dw ? dw->cols : 0, out);
+    const size_t room = ws_bytes - plan.split;
     uint8_t* base = (uint8_t*)ws;
     /* float16: the scales' powers of two apart from the rest of them (see slopes) */
     float *m = std::is_same<T, _Float16>::value ? (float*)(base + plan.m) : nullptr, *parts = (float*)(base + plan.split);
@@ -472,7 +490,7 @@ int run_linear_backward(tc_ctx* ctx, const tc_matrix* dy, const tc_matrix* x, co
         a.factor = by_w && m ? m + 2 : nullptr;
         a.powers = by_w && m ? (const uint16_t*)(base + plan.powers_w) : nullptr;
         a.past = past_caches(dx);
-        TRY((by_w ? multiply<T, false, true, true, false>(ctx, a, parts) : multiply<T, false, false, true, false>(ctx, a, parts)));
+        TRY((by_w ? multiply<T, false, true, true, false>(ctx, a, parts, room) : multiply<T, false, false, true, false>(ctx, a, parts, room)));
     }
     if (dw) {
         ProductArgs a = {};
@@ -486,7 +504,7 @@ int run_linear_backward(tc_ctx* ctx, const tc_matrix* dy, const tc_matrix* x, co
         a.factor = by_x ? m : nullptr;
         a.powers = by_x && m ? (const uint16_t*)(base + plan.powers_x) : nullptr;
         a.past = past_caches(dw);
-        TRY((by_x ? multiply<T, false, true, false, false>(ctx, a, parts) : multiply<T, false, false, false, false>(ctx, a, parts)));
+        TRY((by_x ? multiply<T, false, true, false, false>(ctx, a, parts, room) : multiply<T, false, false, false, false>(ctx, a, parts, room)));
     }
     return TC_OK;
 }
@@ -541,7 +559,7 @@ extern "C" int tc_norm(tc_ctx* ctx, int kind, const tc_matrix* x, const void* d_
 extern "C" int tc_norm_backward_workspace(uint32_t rows, uint32_t cols, size_t* bytes) {
     if (!bytes) return TC_ERR_ARG;
     if (rows > 0x7FFFFFFFu || cols == 0 || cols > TC_NORM_MAX_COLS) return TC_ERR_SHAPE;
-    *bytes = (size_t)norm_back_groups(rows, cols) * 2 * cols * 4;
+    *bytes = (size_t)norm_back_most_groups(rows, cols) * 2 * cols * 4;
     return TC_OK;
 }
 extern "C" int tc_norm_backward(tc_ctx* ctx, int kind, const tc_matrix* dy, const tc_matrix* x, const void* d_gamma, const float* d_mean,
@@ -608,12 +626,13 @@ extern "C" int tc_linear(tc_ctx* ctx, const tc_matrix* x, const tc_matrix* w, co
         TRY(check_shape(ctx, outs[i], x->rows, w->rows));
     }
     TRY(check_vector(ctx, d_bias, 2));
-    size_t need = 0;
-    TRY(tc_linear_workspace(x->rows, x->cols, w->rows, &need));
-    TRY(check_workspace(ctx, d_workspace, workspace_bytes, need));
+    size_t most = 0;
+    TRY(tc_linear_workspace(x->rows, x->cols, w->rows, &most));
+    workspace_bytes = d_workspace ? std::min(workspace_bytes, most) : 0;
+    TRY(check_workspace(ctx, d_workspace, workspace_bytes, workspace_bytes ? 1 : 0));
     if (!x->rows) return TC_OK;
     TRY(ctx_use_device(ctx));
-    return RUN(linear, x->dtype, x, w, d_bias, activation, residual, y, z, d_workspace);
+    return RUN(linear, x->dtype, x, w, d_bias, activation, residual, y, z, d_workspace, workspace_bytes);
 }
 extern "C" int tc_linear_backward_workspace(uint32_t rows, uint32_t in, uint32_t out, size_t* bytes) {
     if (!bytes) return TC_ERR_ARG;
@@ -659,7 +678,7 @@ extern "C" int tc_linear_backward(tc_ctx* ctx, const tc_matrix* dy, const tc_mat
         TRY(check_shape(ctx, x, rows, in));
     }
     TRY(check_vector(ctx, d_dbias, 4));
-    TRY(check_workspace(ctx, d_workspace, workspace_bytes, back_plan(rows, in, out).bytes));
+    TRY(check_workspace(ctx, d_workspace, workspace_bytes, back_plan(rows, in, out).split));
     TRY(ctx_use_device(ctx));
     if (!rows) {
 #if !defined(TC_HOST_EMU)
@@ -668,5 +687,5 @@ extern "C" int tc_linear_backward(tc_ctx* ctx, const tc_matrix* dy, const tc_mat
         return TC_OK;
 #endif
     }
-    return RUN(linear_backward, dy->dtype, dy, x, w, activation, z, dz, dx, dw, d_dbias, d_workspace);
+    return RUN(linear_backward, dy->dtype, dy, x, w, activation, z, dz, dx, dw, d_dbias, d_workspace, workspace_bytes);
 }

@@ -870,3 +870,58 @@ def test_activations_far_below_zero_are_rounded_once(T, ctx, dtype, act, least):
     terms = ref.phi(v) + v.abs() * torch.exp(-0.5 * v * v) / (2.0 * torch.pi) ** 0.5 if act == "gelu" else torch.sigmoid(v) * (1 + v.abs())
     want, e = ref.slope(v, act), rel * terms
     ok(dz[0], want, e + ref.u(t) * (want.abs() + e) + ref.tiny(t))
+
+
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("most,rows,k,n", [(8192, 5370, 11008, 4096), (8192, 4096, 4096, 1024), (16384, 64, 2048, 8), (8192, 300, 1027, 513), (20000, 4096, 4096, 11008), (1, 2100, 1024, 4096)])
+def test_a_workspace_of_other_rows(T, ctx, eight, most, rows, k, n):
+    """Calls in the workspace of a larger call (tc_linear: also of a smaller one, and none), which may be less than their own would be: results within the
+    bounds, nothing written behind it; in a larger one than their own the same bytes."""
+    t = torch.float16
+    seed = rows + k + n
+
+    def room(size):
+        buf = torch.full((size + 256,), 0xAB, dtype=torch.uint8, device="cuda")
+        return buf, buf[:size]
+
+    x, mw, w64 = linear_inputs(T, t, rows, k, n, eight, seed, (0, 0))
+    x64, d64 = x.double(), None
+    z64 = x64 @ w64.t()
+    ez = ref.product_error(x64.abs() @ w64.abs().t(), k)
+    y = torch.empty(rows, n, dtype=t, device="cuda")
+    own = ctx.linear_workspace(rows, k, n)
+    seen = None
+    for size in (0, ctx.linear_workspace(most, k, n), own, own + 4096):
+        buf, work = room(size)
+        ctx.linear(T.Matrix(x), mw, T.Matrix(y), workspace=work if size else None)
+        ctx.sync()
+        ok(y, z64, ez + ref.u(t) * (z64.abs() + ez) + ref.tiny(t))
+        assert (buf[size:] == 0xAB).all()
+        if size >= own:
+            assert seen is None or torch.equal(seen, y)
+            seen = y.clone()
+    del z64, ez
+    if most < rows:
+        return
+    dy = rand((rows, n), seed + 5, t)
+    mx = T.Matrix(x)
+    if eight:
+        q, s = rows8(x)
+        mx, x64 = T.Matrix(q, s), ref.value(q, s)
+    d64 = dy.double()
+    off = (ref.u(t) + 3 * ref.E) * d64.abs() + 2 * ref.tiny(t) if eight else torch.zeros_like(d64)
+    dx, dw = torch.empty(rows, k, dtype=t, device="cuda"), torch.empty(n, k, dtype=t, device="cuda")
+    own = ctx.linear_backward_workspace(rows, k, n)
+    seen = None
+    for size in (ctx.linear_backward_workspace(most, k, n), ctx.linear_backward_workspace(rows, 1, n), own, own + 4096):
+        buf, work = room(size)
+        ctx.linear_backward(T.Matrix(dy), mx, mw, dx=T.Matrix(dx), dw=T.Matrix(dw), workspace=work)
+        ctx.sync()
+        assert (buf[size:] == 0xAB).all()
+        for got, left, e, right, terms in ((dx, d64, off, w64, n), (dw, d64.t(), off.t(), x64, rows)):
+            want, err = left @ right, e @ right.abs()
+            err = err + ref.product_error((left.abs() + e) @ right.abs(), terms)
+            ok(got, want, err + ref.u(t) * (want.abs() + err) + ref.tiny(t))
+        if size >= own:
+            assert seen is None or (torch.equal(seen[0], dx) and torch.equal(seen[1], dw))
+            seen = dx.clone(), dw.clone()
