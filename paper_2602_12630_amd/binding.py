@@ -171,6 +171,7 @@ def load_library(path=None):
         fn.restype = res
         fn.argtypes = args
     L._tc_signatures = sig
+    L._tc_on_gpu = hasattr(L, "hipLaunchKernel")             # a host build is not linked to the HIP runtime
     _LIBS[path] = L
     return L
 
@@ -428,7 +429,7 @@ class Context:
             raise TcError(rc, "tc_ctx_create failed (is a GPU visible?)")
         self.handle = h
         self._vk = {}
-        self._place = int(device) if lib is None else None     # (a host build has the CPU's memory)
+        self._place = int(device) if self.lib._tc_on_gpu else -1      # what get_device() says of tensors that calls may use
 
     def _check(self, rc):
         if rc != TC_OK:
@@ -514,13 +515,13 @@ class Context:
 
     # -- layer operators -----------------------------------------------------------------------
     # dy, x, w, y, z, residual, dx, dz, dw, src and dst are Matrix objects; gamma, beta, bias, mean, rstd, dgamma, dbeta, dbias are
-    # contiguous tensors (16-bit parameters of the activations' type, float32 statistics and sums), all on the context's GPU.
+    # contiguous tensors (16-bit parameters of the activations' type, float32 statistics and sums), all on the context's GPU.  A
+    # tc_matrix by reference will do too; it is taken as it is.
     def _here(self, *matrices):
         place = self._place
-        if place is not None:
-            for m in matrices:
-                if m is not None and m.place != place:
-                    raise ValueError("a matrix that is not on the context's GPU")
+        for m in matrices:
+            if m is not None and getattr(m, "place", place) != place:
+                raise ValueError("a matrix that is not on the context's GPU")
 
     def _vector(self, x, n, dtype):
         """address of n contiguous entries of `dtype` (None: float32, False: any)"""
@@ -528,31 +529,28 @@ class Context:
             return x
         if x.numel() < n or not x.is_contiguous() or not (x.dtype is dtype or dtype is False or dtype is None and str(x.dtype) == "torch.float32"):
             raise ValueError("a vector of %s, %d entries: %s needed, %d side by side" % (x.dtype, x.numel(), dtype or "torch.float32", n))
-        if self._place is not None and x.get_device() != self._place:
+        if x.get_device() != self._place:
             raise ValueError("a vector that is not on the context's GPU")
         return x.data_ptr()
 
     def _room(self, x):
         if x is None:
             return None, 0
-        if self._place is not None and x.get_device() != self._place or not x.is_contiguous():
+        if x.get_device() != self._place or not x.is_contiguous():
             raise ValueError("a workspace is a contiguous tensor on the context's GPU")
         return x.data_ptr(), x.numel() * x.element_size()
 
     def checkpoint_encode(self, src, dst):
         """dst (int8 rows, scales) = the 8-bit form of src's rows"""
-        if self._place is not None and not src.place == dst.place == self._place:
-            self._here(src, dst)
+        self._here(src, dst)
         self._check(self.lib.tc_checkpoint_encode(self.handle, src, dst))
 
     def checkpoint_decode(self, src, dst):
-        if self._place is not None and not src.place == dst.place == self._place:
-            self._here(src, dst)
+        self._here(src, dst)
         self._check(self.lib.tc_checkpoint_decode(self.handle, src, dst))
 
     def norm(self, kind, x, gamma, beta, eps, y, mean=None, rstd=None):
-        if self._place is not None and not x.place == y.place == self._place:
-            self._here(x, y)
+        self._here(x, y)
         rows, cols, t = getattr(y, "form", _BARE)
         self._check(self.lib.tc_norm(self.handle, kind, x, self._vector(gamma, cols, t), self._vector(beta, cols, t), eps, y,
                                      self._vector(mean, rows, None), self._vector(rstd, rows, None)))

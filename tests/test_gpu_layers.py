@@ -925,3 +925,42 @@ def test_a_workspace_of_other_rows(T, ctx, eight, most, rows, k, n):
         if size >= own:
             assert seen is None or (torch.equal(seen[0], dx) and torch.equal(seen[1], dw))
             seen = dx.clone(), dw.clone()
+
+
+def test_calls_of_the_binding_without_a_matrix(T, ctx):
+    """None, or a tc_matrix by reference, where a Matrix is expected: what the library says of them"""
+    import ctypes
+
+    t = torch.float16
+    x, q, s = rand((4, 8), 1, t), torch.empty(4, 8, dtype=torch.int8, device="cuda"), torch.empty(4, device="cuda")
+    m, m8, w = T.Matrix(x), T.Matrix(q, s), T.Matrix(rand((8, 8), 2, t))
+    v, work = torch.ones(8, device="cuda"), space(1 << 20)
+    for call in (lambda: ctx.checkpoint_encode(None, m8), lambda: ctx.checkpoint_encode(m, None), lambda: ctx.checkpoint_decode(None, m), lambda: ctx.checkpoint_decode(m8, None),
+                 lambda: ctx.norm(0, None, None, None, 1e-5, m), lambda: ctx.norm(0, m, v.to(t), None, 1e-5, None), lambda: ctx.norm_backward(1, None, m, None, None, v, m, None, None, None),
+                 lambda: ctx.norm_backward(1, m, None, None, None, v, m, None, None, None), lambda: ctx.linear(None, w, m), lambda: ctx.linear(m, None, m),
+                 lambda: ctx.linear(m, w, None), lambda: ctx.linear_backward(None, m, w, dx=m, workspace=work), lambda: ctx.linear_backward(m, m, None, dx=m, workspace=work)):
+        with pytest.raises(T.TcError) as e:
+            call()
+        assert e.value.code == T.binding.TC_ERR_ARG
+    by = lambda a: ctypes.byref(a.view)  # noqa: E731
+    ctx.checkpoint_encode(by(m), by(m8))
+    y, back = torch.empty_like(x), torch.empty_like(x)
+    ctx.norm(1, by(m), None, None, 1e-5, by(T.Matrix(y)))
+    ctx.checkpoint_decode(by(m8), by(T.Matrix(back)))
+    ctx.sync()
+    want, scale = ref.encode(x)
+    assert torch.equal(q, want) and torch.equal(s, scale)
+    v64 = ref.value(want, scale)
+    ok(back, v64, (ref.u(t) + 2 * ref.E) * v64.abs() + ref.tiny(t))
+    y64, _, rstd = ref.norm(x.double(), None, None, 1e-5, False)
+    ok(y, y64, ref.norm_bound(x.double(), None, None, y64, rstd, t, False))
+
+
+def test_a_library_that_is_named_is_checked_too(T):
+    c = T.Context(0, None, T.load_library(T.binding.library_path()))
+    near, far = (T.Matrix(torch.zeros(4, 8, dtype=torch.float16, device=d)) for d in ("cuda", "cpu"))
+    for call in (lambda: c.norm(1, far, None, None, 1e-5, near), lambda: c.norm(1, near, None, None, 1e-5, far), lambda: c.norm(1, near, torch.ones(8, dtype=torch.float16), None, 1e-5, near),
+                 lambda: c.linear(near, T.Matrix(torch.zeros(8, 8, dtype=torch.float16, device="cuda")), near, workspace=torch.zeros(64, dtype=torch.uint8))):
+        with pytest.raises(ValueError):
+            call()
+    c.close()
