@@ -156,12 +156,21 @@ struct tc_vk {
 /* ======================================================================================= */
 /* helpers                                                                                 */
 /* ======================================================================================= */
+/* (without memory for the message the code alone comes back: nothing is thrown across the C boundary) */
 static int fail(tc_ctx* ctx, int code, const char* msg) {
-    if (ctx) ctx->err = msg;
+    try {
+        if (ctx) ctx->err = msg;
+    } catch (...) {
+        ctx->err.clear();
+    }
     return code;
 }
 static int fail_hip(tc_ctx* ctx, int e, const char* where) {
-    if (ctx) ctx->err = std::string(where) + ": " + rt::error_string(e);
+    try {
+        if (ctx) ctx->err = std::string(where) + ": " + rt::error_string(e);
+    } catch (...) {
+        ctx->err.clear();
+    }
     return TC_ERR_HIP;
 }
 #define RT(call)                                             \
