@@ -964,3 +964,72 @@ def test_a_library_that_is_named_is_checked_too(T):
         with pytest.raises(ValueError):
             call()
     c.close()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,cols", [(5, 7), (300, 515), (1100, 2051), (40, 4099), (1030, 8190), (9, 12295), (6, 32767), (1500, 16392)])
+def test_norms_in_the_place_of_their_input(T, ctx, dtype, rows, cols):
+    t = ref.DT[dtype]
+    for kind in (T.TC_NORM_LAYER, T.TC_NORM_RMS):
+        x, dy, y, dx = (strided(rand((rows, cols), 3 + i, t), 1, 2)[1] for i in range(4))
+        mean, rstd = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+        ctx.norm(kind, T.Matrix(x), None, None, 1e-5, T.Matrix(y), mean, rstd)
+        ctx.norm_backward(kind, T.Matrix(dy), T.Matrix(x), None, mean, rstd, T.Matrix(dx), None, None, None)
+        ctx.norm_backward(kind, T.Matrix(dy), T.Matrix(x), None, mean, rstd, T.Matrix(dy), None, None, None)
+        ctx.norm(kind, T.Matrix(x), None, None, 1e-5, T.Matrix(x))
+        ctx.sync()
+        assert torch.equal(x, y) and torch.equal(dy, dx)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,k,n", [(5, 64, 40), (70, 65, 33), (487, 4104, 4104), (8200, 136, 8456), (8456, 520, 8200), (10248, 8200, 520)])
+def test_products_in_the_place_of_their_input(T, ctx, dtype, rows, k, n):
+    t = ref.DT[dtype]
+    x, w, residual, y = rand((rows, k), 1, t), rand((n, k), 2, t, k ** -0.5), rand((rows, n), 3, t), torch.empty(rows, n, dtype=t, device="cuda")
+    work = space(max(ctx.linear_workspace(rows, k, n), ctx.linear_backward_workspace(rows, k, n)))
+    ctx.linear(T.Matrix(x), T.Matrix(w), T.Matrix(y), activation=3, residual=T.Matrix(residual), workspace=work)
+    ctx.linear(T.Matrix(x), T.Matrix(w), T.Matrix(residual), activation=3, residual=T.Matrix(residual), workspace=work)
+    ctx.sync()
+    assert torch.equal(residual, y)
+    z8, w8, dy, dz = rows8(rand((rows, n), 4, t)), rows8(w), rand((rows, n), 5, t), torch.empty_like(y)
+    dx, again = torch.empty_like(x), torch.empty_like(x)
+    ctx.linear_backward(T.Matrix(dy), None, T.Matrix(*w8), 2, T.Matrix(*z8), T.Matrix(dz), T.Matrix(dx), workspace=work)
+    ctx.linear_backward(T.Matrix(dy), None, T.Matrix(*w8), 2, T.Matrix(*z8), T.Matrix(dy), T.Matrix(again), workspace=work)
+    ctx.sync()
+    assert torch.equal(dy, dz) and torch.equal(dx, again)
+
+
+def test_large_products_captured_and_replayed(T):
+    """the kernels of the largest tiles, int8 operands widened, in a graph that is replayed on new inputs between eager calls"""
+    t = torch.bfloat16
+    stream = torch.cuda.Stream()
+    c = T.Context(0, stream.cuda_stream)
+    rows, k, n = 4096, 2048, 4104
+    x, w8, dy = rand((rows, k), 1, t), rows8(rand((n, k), 2, t, k ** -0.5)), rand((rows, n), 3, t)
+    x8 = rows8(x)
+    y, dx, dw = (torch.empty(*s, dtype=t, device="cuda") for s in ((rows, n), (rows, k), (n, k)))
+    work = space(max(c.linear_workspace(rows, k, n), c.linear_backward_workspace(rows, k, n)))
+    mx, mw, my, mdy, mx8, mdx, mdw = T.Matrix(x), T.Matrix(*w8), T.Matrix(y), T.Matrix(dy), T.Matrix(*x8), T.Matrix(dx), T.Matrix(dw)
+
+    def calls():
+        c.linear(mx, mw, my, activation=2, workspace=work)
+        c.linear_backward(mdy, mx8, mw, dx=mdx, dw=mdw, workspace=work)
+
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        calls()
+    for i in range(3):
+        x.copy_(rand((rows, k), 10 + i, t))
+        dy.copy_(rand((rows, n), 20 + i, t))
+        torch.cuda.synchronize()
+        calls()
+        torch.cuda.synchronize()
+        want = [o.clone() for o in (y, dx, dw)]
+        for o in (y, dx, dw, work):
+            o.fill_(3)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(want, (y, dx, dw))), i
+    c.close()
