@@ -231,14 +231,15 @@ int tc_encode_batch_scaled(tc_ctx* ctx, int count, const void* const* d_src, con
  *
  * A prover commits to what a layer's products and norms have made.  These calls are those passes, for tensors that stay
  * where the commitment reads them: 16-bit activations, weights in 16 bits or as the committed int8 rows, and activations
- * kept for a backward pass in 8 bits, in the form that tc_commit takes (TC_I8), so that a commitment binds the very bytes
- * that the gradients were taken from.
+ * kept for a backward pass in 8 bits, in the form that tc_commit takes (TC_I8), so that a commitment binds the very rows
+ * that the gradients were taken from.  It binds the whole numbers alone: the values are scale * q, and the scales of the rows are bound
+ * by a commitment of their own (their bytes are a tensor of TC_I8, rows x 4).
  *
  * All of them are asynchronous on the context's stream, allocate nothing, read nothing back and may be captured into a
  * graph; scratch memory is the caller's (the *_workspace calls say how much, for every type and choice of outputs).  A workspace that is large enough for
  * some number of rows serves calls of fewer rows (of the same columns) too.  The same call on the same data gives the same bytes, every time: no
  * sum depends on the order in which workgroups run.  Sums, statistics and products are held in 32 bits; results are
- * rounded once to their type.  Outputs may not overlap inputs or one another, but for: y in the place of the residual
+ * rounded once to their type, but that the gradient before the activation is rounded to 16 bits before dx and dw are formed from it (tc_linear_backward).  Outputs may not overlap inputs or one another, but for: y in the place of the residual
  * (tc_linear), y in the place of x (tc_norm), dx in the place of dy (tc_norm_backward), dz in the place of dy
  * (tc_linear_backward).  Two calls that overlap in time (on several streams, or as replayed graphs) need a workspace each. */
 
@@ -283,7 +284,7 @@ int tc_norm_backward_workspace(uint32_t rows, uint32_t cols, size_t* bytes);
 
 /* z = x w^T + bias,  y = act(z) + residual.  x: rows x in, 16 bits; w: out x in, of x's type or TC_I8 with its scales (the
  * rows as they are committed); d_bias: out values of x's type or NULL; residual and z: rows x out of x's type or NULL; y the same.
- * TC_ACT_GELU is z Phi(z), Phi the normal distribution's integral; TC_ACT_SILU is z / (1 + exp(-z)). */
+ * TC_ACT_GELU is z Phi(z), Phi the normal distribution's integral; TC_ACT_SILU is z / (1 + exp(-z)).  Values of less than 10^-36 may come out as 0. */
 #define TC_ACT_NONE 0
 #define TC_ACT_RELU 1
 #define TC_ACT_GELU 2
@@ -295,7 +296,10 @@ int tc_linear(tc_ctx* ctx, const tc_matrix* x, const tc_matrix* w, const void* d
 int tc_linear_workspace(uint32_t rows, uint32_t in, uint32_t out, size_t* bytes);
 /* Its gradients:  dz = dy act'(z),  dx = dz w,  dw = dz^T x,  dbias = sum over rows of dz (relu'(0) = 0; the residual's gradient is dy itself).
  * z and x: as the forward pass had them, in 16 bits or as checkpoints; w as there.  With an activation z and dz are needed; without one
- * both must be NULL and dz is dy.  x may be NULL without dw, w without dx.  dz, dx, dw have dy's type; d_dbias: out float32.  dx, dw
+ * both must be NULL and dz is dy.  dx and dw are formed from dz as it is returned; an int8 operand's scale is put into dz before that, so there they
+ * are formed from dz times the scale, rounded to dy's type: either way each term carries at most half a step of that type, below its normal range
+ * half the smallest step.  (float16 takes the scale's part beside a power of two, so that rows lose nothing beside others whose scale is up to 2^32 times
+ * theirs; the smallest step counts whole there.)  x may be NULL without dw, w without dx.  dz, dx, dw have dy's type; d_dbias: out float32.  dx, dw
  * and d_dbias may be NULL. */
 int tc_linear_backward(tc_ctx* ctx, const tc_matrix* dy, const tc_matrix* x, const tc_matrix* w, int activation, const tc_matrix* z,
                        const tc_matrix* dz, const tc_matrix* dx, const tc_matrix* dw, float* d_dbias, void* d_workspace,

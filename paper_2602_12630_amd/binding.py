@@ -564,13 +564,13 @@ class Context:
                                               *self._room(workspace)))
 
     def linear(self, x, w, y, bias=None, activation=TC_ACT_NONE, residual=None, z=None, workspace=None):
-        """workspace: a uint8 tensor of linear_workspace(rows, in, out) bytes"""
+        """workspace: a uint8 tensor of linear_workspace(rows, in, out) bytes; with less, or none, the call is slower"""
         self._here(x, w, y, residual, z)
         _, out, t = getattr(y, "form", _BARE)
         self._check(self.lib.tc_linear(self.handle, x, w, self._vector(bias, out, t), activation, residual, y, z, *self._room(workspace)))
 
     def linear_backward(self, dy, x, w, activation=TC_ACT_NONE, z=None, dz=None, dx=None, dw=None, dbias=None, workspace=None):
-        """workspace: a uint8 tensor of linear_backward_workspace(rows, in, out) bytes"""
+        """workspace: a uint8 tensor of linear_backward_workspace(rows, in, out) bytes, or one for more rows"""
         self._here(dy, x, w, z, dz, dx, dw)
         _, out, _ = getattr(dy, "form", _BARE)
         self._check(self.lib.tc_linear_backward(self.handle, dy, x, w, activation, z, dz, dx, dw, self._vector(dbias, out, None),

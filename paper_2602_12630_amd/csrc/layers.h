@@ -20,7 +20,7 @@ template <class T> struct Vec {
  * The upper tail of the normal distribution is exp(-a^2 / 2) R(a), where R falls slowly from 1/2 to 0.4 / a: t times a polynomial of degree 7 in
  * t = 1 / (1 + 0.3 a), whose coefficients make the largest relative error over 0 <= a <= 13.5 least (1.3e-7; found by linear programming over 3000 points; with float32
  * roundings 4.3e-7).  So values far below zero are rounded to their type once too, down to float32's normal range, where the tail becomes 0 (z < -13.2).  gelu = max(z, 0) - |z| tail: some
- * 25 operations, where the library's erf alone takes 40; in the epilogue of a product of 8192 x 4096 -> 11008 they add some 60 us to 640.  |z| is held at 14, beyond
+ * 25 operations, where the library's erf alone takes 40; in the epilogue of a product of 8192 x 4096 -> 11008 (z kept) they add 56 us to 618.  |z| is held at 14, beyond
  * which every factor has become 0, so that infinities (values before the activation that overflowed) do not turn into NaNs; NaNs stay. */
 __device__ __forceinline__ float held_at_14(float z) {
     const float a = fabsf(z);

@@ -1033,3 +1033,26 @@ def test_large_products_captured_and_replayed(T):
         torch.cuda.synchronize()
         assert all(torch.equal(p, q) for p, q in zip(want, (y, dx, dw))), i
     c.close()
+
+
+def test_the_scales_of_a_checkpoint_are_committed_as_their_bytes(T, ctx):
+    """a commitment of the rows binds the whole numbers alone; one of the scales' bytes binds what they stand for"""
+    from gpu_util import TAU_BYTES, pps
+    from oracle import bls12_381 as ec
+    from oracle import cbind
+
+    rows, cols = 12, 40
+    x = rand((rows, cols), 1, torch.float16)
+    q, s = torch.empty(rows, cols, dtype=torch.int8, device="cuda"), torch.empty(rows, device="cuda")
+    ctx.checkpoint_encode(T.Matrix(x), T.Matrix(q, s))
+    ctx.sync()
+    q2, s2 = torch.empty_like(q), torch.empty_like(s)
+    ctx.checkpoint_encode(T.Matrix(x * 2), T.Matrix(q2, s2))
+    ctx.sync()
+    commitments = []
+    for tensor in (q, q2, s.view(torch.int8).view(rows, 4), s2.view(torch.int8).view(rows, 4)):
+        srs = ctx.setup_from_trapdoor(TAU_BYTES, tuple(tensor.shape), T.TC_SRS_SUFFIX)
+        commitments.append(ctx.commit(srs, tensor, T.TC_I8))
+        assert commitments[-1] == ec.g1_to_bytes(cbind.commit(pps(tuple(tensor.shape)), tensor.cpu().numpy()))
+        srs.close()
+    assert commitments[0] == commitments[1] and commitments[2] != commitments[3]
