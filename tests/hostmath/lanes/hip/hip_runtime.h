@@ -1,6 +1,6 @@
 // What layers.h and tc_layers.cpp need of HIP to be compiled for the host and run lane by lane, for the addresses that they form: every load and
 // store is made, on memory that the sanitizer watches.  Nothing passes between lanes (a sum over them is a lane's own value, a matrix instruction returns its
-// sums as they were), so that results mean nothing.
+// sums as they were), so that results mean nothing; LDS that a lane has not written itself holds zeros (the compiler's -ftrivial-auto-var-init=zero).
 #pragma once
 #include <math.h>
 #include <stddef.h>

@@ -52,7 +52,7 @@ static const char* what = "";
 /* a block of n bytes, and nothing beside it */
 struct Block {
     std::unique_ptr<uint8_t[]> p;
-    explicit Block(size_t n) : p(new uint8_t[n ? n : 1]) {}
+    explicit Block(size_t n) : p(new uint8_t[n ? n : 1]()) {}
     void* at(size_t i = 0) { return p.get() + i; }
 };
 /* rows x cols with a stride, beginning `shift` elements into its block */
@@ -65,10 +65,12 @@ struct Mat {
         const size_t size = dtype == TC_I8 ? 1 : 2;
         bytes = (rows ? (size_t)(rows - 1) * (cols + gap) + cols + shift : 0) * size;
         m = {data.at(shift * size), dtype == TC_I8 ? (float*)scale.at() : nullptr, rows, cols, cols + gap, dtype};
-        for (size_t i = 0; i < bytes; i += size) {
+        const size_t some = std::min<size_t>(bytes, 100002);
+        for (size_t i = 0; i < some; i += size) {
             if (size == 1) ((int8_t*)data.at())[i] = (int8_t)gen();
             else ((uint16_t*)data.at())[i / 2] = (uint16_t)(0x3800 + gen() % 1024);
         }
+        for (size_t i = some; i < bytes; i += some) memcpy(data.at(i), data.at(), std::min(some, bytes - i));
         if (dtype == TC_I8)
             for (uint32_t r = 0; r < rows; ++r) m.d_scale[r] = 0.01f * (1 + gen() % 100);
         if (gap * size >= 16)
@@ -77,11 +79,10 @@ struct Mat {
     }
     /* outputs: every entry has to be written, where all workgroups were run */
     void clear() {
-        for (uint32_t r = 0; r < m.rows; ++r)
-            for (uint32_t c = 0; c < m.cols; ++c) {
-                if (m.dtype == TC_I8) ((int8_t*)m.d_data)[r * m.ld + c] = -128;
-                else ((uint16_t*)m.d_data)[r * m.ld + c] = 0x7EAD;
-            }
+        for (uint32_t r = 0; r < m.rows; ++r) {
+            if (m.dtype == TC_I8) memset((int8_t*)m.d_data + r * m.ld, -128, m.cols);
+            else std::fill_n((uint16_t*)m.d_data + r * m.ld, m.cols, 0x7EAD);
+        }
     }
     void written(const char* name) const {
         if (lanes::skipped) return;
@@ -245,15 +246,15 @@ int main() {
                                      {3, 8199}, {2, 16384}, {3, 16385}, {2, 16390}, {2, 32768}, {3, 32767}, {2, 40001}};
     for (auto& s : row_sizes)
         for (uint32_t shift : {0u, 1u, 8u})
-            for (int dtype : {TC_F16, TC_BF16}) checkpoints_and_norms(s[0], s[1], dtype, shift * 2, shift);
+            checkpoints_and_norms(s[0], s[1], (s[0] + shift) % 2 ? TC_F16 : TC_BF16, shift * 2, shift);
     puts("rows");
-    lanes::most_blocks = 40;
+    lanes::most_blocks = 24;
     const uint32_t sizes[][3] = {{1, 1, 1}, {1, 64, 128}, {2, 65, 7}, {3, 63, 130}, {8, 80, 40}, {9, 16, 24}, {16, 512, 96}, {17, 72, 129}, {16, 8, 264}, {65, 1027, 33}, {129, 640, 264}, {5, 5, 300},
                                  {9, 24, 515}, {5, 1025, 1030}, {70, 129, 513}, {3, 9, 1031}, {300, 328, 392}, {200, 200, 4104}, {300, 4104, 520}, {487, 1032, 1096}, {1100, 2056, 520}};
     for (auto& s : sizes)
         for (uint32_t shift : {0u, 1u, 8u})
             for (int eight = 0; eight < 2; ++eight)
-                for (int dtype : {TC_F16, TC_BF16}) products(s[0], s[1], s[2], dtype, eight, shift * 2, shift, (s[0] + shift + eight) % 4, shift == 8);
+                products(s[0], s[1], s[2], eight || (s[0] + shift) % 2 ? TC_F16 : TC_BF16, eight, shift * 2, shift, (s[0] + shift + eight) % 4, shift == 8);
     puts("products");
     lanes::most_blocks = 2;
     const uint32_t large[][3] = {{8200, 136, 8456}, {8456, 520, 8200}, {520, 8200, 8456}, {4104, 1040, 1040}, {4100, 1043, 2049}};

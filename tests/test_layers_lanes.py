@@ -1,4 +1,4 @@
-"""The layer operators' kernels and launches on the CPU, lane by lane under AddressSanitizer and UBSan (tests/hostmath/layers_lanes.cpp): every address
+"""The layer operators' kernels and launches on the CPU, lane by lane under AddressSanitizer and UBSan's checks of alignment, bounds and overflow (tests/hostmath/layers_lanes.cpp): every address
 that they form lies in its block, every output entry is written, and the tiles of the products hold what belongs there."""
 import os
 import subprocess
@@ -15,8 +15,8 @@ def test_layer_kernels_stay_inside_their_buffers(tmp_path):
     if not os.path.exists(CLANG):
         pytest.skip("the kernels' vector types want clang")
     exe = str(tmp_path / "layers_lanes")
-    cmd = [CLANG, "-x", "c++", "-O1", "-gline-tables-only", "-std=c++17", "-fsanitize=address,undefined", "-fno-sanitize=vptr,function,float-cast-overflow,shift-base",
-           "-fno-sanitize-recover=undefined", "-Wno-everything", "-I", os.path.join(HERE, "lanes"), "-o", exe, os.path.join(HERE, "layers_lanes.cpp")]
+    cmd = [CLANG, "-x", "c++", "-O1", "-gline-tables-only", "-std=c++17", "-fsanitize=address,alignment,bounds,signed-integer-overflow",
+           "-fno-sanitize-recover=all", "-ftrivial-auto-var-init=zero", "-Wno-everything", "-I", os.path.join(HERE, "lanes"), "-o", exe, os.path.join(HERE, "layers_lanes.cpp")]
     built = subprocess.run(cmd, capture_output=True, text=True, cwd=ROOT)
     if built.returncode != 0 and "libclang_rt" in built.stderr:
         pytest.skip("the sanitizer runtimes are not installed")
